@@ -319,6 +319,74 @@ int32_t cake_decode_step(cake_ctx* ctx, int32_t layer, const void* q_new, const 
 int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t* positions_out,
                               float* scores_out, int32_t* slots_out, void* stream);
 
+/* ---- attention beside the eviction path ------------------------------------------------
+ * The attention whose keys the calls above score, shrink and pack: of whole prompts (Section 2, Eq. 2),
+ * of new tokens over what was retained, and the attention weight that keys have accumulated (the
+ * indicator of the heavy-hitter method in the paper's compatibility study, Section 5.3).  The scale is
+ * 1 / sqrt(d).  Softmax statistics, sums and outputs are held in fp32 and rounded once at the end.
+ * These calls do not advance the context's batch: they may come at any point of it, on any stream, and
+ * several times.  They allocate nothing, synchronise nothing, and a stream capture may record them.
+ * Tensors must start on 16-byte boundaries, and the context's device must be the current one, else
+ * CAKE_ERR_ARG. */
+
+/* Causal attention over the prompts of the current batch (cake_begin), one layer:
+ *   O_i = sum_{j <= i} softmax_j(q_i . k_j / sqrt(d)) v_j   inside each request,
+ * query head h reading KV head h / G.
+ *   q     H_q * T rows of d elements: row (h, t) at q + h * q_head_stride + t * q_token_stride
+ *         ([H_q][T][d]: T*d and d; [T][H_q][d]: d and H_q*d).  Strides in elements, their
+ *         bytes multiples of 16, not negative
+ *   k, v  [H_kv][T][d] (packed varlen, as cake_score_layer and cake_compact take them)
+ *   out   as q, with strides of its own under which no two rows overlap; must not overlap the inputs
+ *   lse   optional [H_q][T] fp32: natural-log sum-exp of each row's scaled logits
+ *   lse_window  optional [n_req][H_q][S_w] fp32: the same of the last S_w rows of every request, as
+ *         cake_score_layer takes it (its scoring is then one pass instead of two)
+ * What lies behind a row (later tokens, other requests) has no influence on it, not even an infinity or
+ * a NaN there. */
+int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
+                           const void* k, const void* v, void* out, int64_t out_head_stride,
+                           int64_t out_token_stride, float* lse, float* lse_window, void* stream);
+
+/* Attention weight that every key of the current batch's prompts has received from all queries of its
+ * request, averaged over the query heads of its KV head:
+ *   A_j = 1/G sum_h sum_{i >= j} exp(q_hi . k_j / sqrt(d) - lse_hi)
+ * q, k and lse as in cake_attend_prompt (lse as that call leaves it); out [H_kv][T] fp32.  For an eviction by
+ * accumulated attention hand it to cake_set_indicators (with preferences from cake_set_preferences).  The sums do
+ * not depend on scheduling: a call repeats bit for bit. */
+int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
+                                  const void* k, const float* lse, float* out, void* stream);
+
+/* Attention of one new token per request over the cached rows of one layer.  The context gives the shapes
+ * and types alone (L, H_q, H_kv, d, dtype), not its batch: it may meanwhile work on other prompts, and calls
+ * on several streams may run side by side, each with a workspace of its own.
+ *   q            [n_req][H_q][d], n_req <= 65535
+ *   k_cache, v_cache, row_offsets  as cake_compact or cake_decode_begin wrote them: block (r,l) is rows
+ *                row_offsets[r*L+l] .. row_offsets[r*L+l+1]-1, [H_kv][len][d]; offsets are read on the device.
+ *                (After a cake_decode_step every slot of a block holds a row that the step's token has seen,
+ *                the evicted one among them: this call then gives that token's attention output.)
+ *   k_tail, v_tail, tail_len, tail_capacity  rows of tokens generated since the compaction, the new one
+ *                included: device [n_req][H_kv][tail_capacity][d], of which request r's first tail_len[r]
+ *                (device int32, taken as 0 .. tail_capacity) are attended; what lies behind has no
+ *                influence.  tail_capacity 0: none, the pointers are not read
+ *   out          [n_req][H_q][d]; a request without any row gives zeros
+ *   lse          optional [n_req][H_q] fp32, natural log; -inf without any row
+ *   workspace    device, cake_attend_workspace_bytes(ctx, n_req) at least; its contents need no
+ *                initialisation and are not kept.  Calls that may overlap need one each (two captured
+ *                graphs that are replayed side by side, for instance) */
+int64_t cake_attend_workspace_bytes(const cake_ctx* ctx, int32_t n_req);
+int32_t cake_attend_cache(const cake_ctx* ctx, int32_t n_req, int32_t layer, const void* q, const void* k_cache,
+                          const void* v_cache, const int64_t* row_offsets, const void* k_tail,
+                          const void* v_tail, const int32_t* tail_len, int64_t tail_capacity, void* out,
+                          float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+/* The same over the 4-bit rows that cake_compact_int4 wrote with `group`: a key is k_zero + code * k_scale of its
+ * channel and row group, a value v_zero + code * v_scale of its row and channel group.  Tail rows are in the
+ * context's dtype. */
+int32_t cake_attend_int4(const cake_ctx* ctx, int32_t n_req, int32_t layer, const void* q,
+                         const uint8_t* k_codes, const float* k_scale, const float* k_zero,
+                         const uint8_t* v_codes, const float* v_scale, const float* v_zero, int32_t group,
+                         const int64_t* row_offsets, const int64_t* kgroup_offsets, const void* k_tail,
+                         const void* v_tail, const int32_t* tail_len, int64_t tail_capacity, void* out,
+                         float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Bound, in SM clock cycles, of every wait inside the kernels (a CTA waiting for another CTA's
  * partial results, or for one of its own barriers).  A wait that runs out sets the sticky device
  * status CAKE_ERR_TIMEOUT; the kernel then drains and returns, and the context stays usable (the

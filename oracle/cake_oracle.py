@@ -401,6 +401,55 @@ def pack_nibbles(codes: np.ndarray) -> np.ndarray:
 
 
 # --------------------------------------------------------------------------
+# attention over prompts and caches                          (Section 2, Eq. 2)
+# --------------------------------------------------------------------------
+def attend(q: np.ndarray, k: np.ndarray, v: np.ndarray, visible=None):
+    """One head: q [M][d] over k, v [N][d]; `visible` [M][N] (default: all).  Returns (out [M][d], lse [M], spread [M][d])
+    with spread = sum_j p_j |v_j|, the scale of a rounding of the weights.  A row that sees nothing gives zeros and
+    an lse of -inf.  What a row does not see has no influence, not even an infinity or a NaN."""
+    q, k, v = (np.asarray(x, dtype=F64) for x in (q, k, v))
+    out, spread = np.zeros((q.shape[0], v.shape[1])), np.zeros((q.shape[0], v.shape[1]))
+    lse = np.full(q.shape[0], -np.inf)
+    for i in range(q.shape[0]):
+        seen = np.ones(k.shape[0], dtype=bool) if visible is None else visible[i]
+        if not seen.any():
+            continue
+        s = k[seen] @ q[i] / np.sqrt(F64(q.shape[1]))
+        top = s.max()
+        e = np.exp(s - top)
+        lse[i] = top + np.log(e.sum())
+        p = e / e.sum()
+        out[i], spread[i] = p @ v[seen], p @ np.abs(v[seen])
+    return out, lse, spread
+
+
+def prompt_attention(q: np.ndarray, k: np.ndarray, v: np.ndarray):
+    """Causal attention of one request, q [H_q][N][d], k, v [H_kv][N][d]: out, lse, spread of every head."""
+    G = q.shape[0] // k.shape[0]
+    causal = np.tril(np.ones((q.shape[1], q.shape[1]), dtype=bool))
+    parts = [attend(q[h], k[h // G], v[h // G], causal) for h in range(q.shape[0])]
+    return tuple(np.stack(x) for x in zip(*parts))
+
+
+def unpack_nibbles(packed: np.ndarray) -> np.ndarray:
+    """Inverse of pack_nibbles."""
+    out = np.empty((packed.shape[0], packed.shape[1] * 2), dtype=np.uint8)
+    out[:, 0::2], out[:, 1::2] = packed & 15, packed >> 4
+    return out
+
+
+def dequantize_keys(codes: np.ndarray, scale: np.ndarray, zero: np.ndarray, group: int) -> np.ndarray:
+    """Rows of one head from codes [len][d] and scale, zero [ceil(len/group)][d]."""
+    at = np.arange(codes.shape[0]) // group
+    return zero.astype(F64)[at] + codes * scale.astype(F64)[at]
+
+
+def dequantize_values(codes: np.ndarray, scale: np.ndarray, zero: np.ndarray, group: int) -> np.ndarray:
+    """Rows from codes [len][d] and scale, zero [len][d/group]."""
+    return np.repeat(zero.astype(F64), group, axis=1) + codes * np.repeat(scale.astype(F64), group, axis=1)
+
+
+# --------------------------------------------------------------------------
 # decode-time eviction        (Section 5.1 "Implementation Details"; Appendix
 #                              "More Implementation Details"; Listing 1, the
 #                              branches taken when not prefilling)

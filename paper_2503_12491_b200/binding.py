@@ -33,7 +33,8 @@ EXPORTS = [
     "cake_profile_enable", "cake_profile_read", "cake_uses_tensor_cores",
     "cake_select_positions_static", "cake_plan_info", "cake_set_wait_limit", "cake_debug_skew_sync",
     "cake_decode_rows_bound", "cake_decode_begin", "cake_decode_step", "cake_decode_get_state",
-    "cake_compact_int4", "cake_plan_check", "cake_clear_unused",
+    "cake_compact_int4", "cake_plan_check", "cake_clear_unused", "cake_attend_prompt",
+    "cake_accumulate_attention", "cake_attend_workspace_bytes", "cake_attend_cache", "cake_attend_int4",
 ]
 PROF_KINDS = ["score", "finalize", "allocate", "evict", "compact"]
 
@@ -104,6 +105,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cake_decode_begin.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp, vp, vp, i32, vp]
     lib.cake_decode_step.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
     lib.cake_decode_get_state.argtypes = [vp, i32, i32, vp, vp, vp, vp]
+    lib.cake_attend_prompt.argtypes = [vp, vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, vp]
+    lib.cake_accumulate_attention.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp]
+    lib.cake_attend_workspace_bytes.argtypes = [vp, i32]
+    lib.cake_attend_workspace_bytes.restype = i64
+    lib.cake_attend_cache.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+    lib.cake_attend_int4.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp,
+                                     i64, vp]
     lib.cake_set_wait_limit.argtypes = [vp, i64]
     lib.cake_debug_skew_sync.argtypes = [vp, i32]
     lib.cake_strerror.argtypes = [i32]
@@ -113,7 +121,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("cake_packed_rows_bound", "cake_strerror", "cake_launch_count",
-                        "cake_decode_rows_bound"):
+                        "cake_decode_rows_bound", "cake_attend_workspace_bytes"):
             fn.restype = i32
     fast = _load_native()
     fast.init(path)
@@ -358,6 +366,57 @@ class Cake:
         sl = torch.empty(H, length, dtype=torch.int32, device="cuda")
         _check(_fast.decode_get_state(self._a, req, layer, pos, sc, sl), "cake_decode_get_state")
         return pos, sc, sl
+
+    # -- attention over prompts and caches
+    def attend_prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, lse_window: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Causal attention over the prompts of the current batch: (out, lse).
+
+        q: [H_q][T][d] with any strides between heads and tokens (a transposed [T][H_q][d] as a projection leaves
+        it); k, v: contiguous [H_kv][T][d].  `out` has q's shape (default: q's layout); `lse` is [H_q][T] fp32;
+        `lse_window`, if given, receives the window rows' [n_req][H_q][S_w] as score_layer takes them."""
+        c = self.cfg
+        rc, out, lse = _fast.attend_prompt(self._a, self._fp32, self.n_req, self.total_tokens, c.n_q_heads, c.n_kv_heads,
+                                           c.head_dim, c.window, q, k, v, out, lse, lse_window)
+        _check(rc, "cake_attend_prompt")
+        return out, lse
+
+    def accumulate_attention(self, q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor,
+                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention weight every key has received from all queries of its prompt, averaged over the query heads of its
+        KV head: [H_kv][T] fp32, as set_indicators takes it.  q, k as in attend_prompt, lse as it returns it."""
+        c = self.cfg
+        rc, out, _ = _fast.accumulate_attention(self._a, self._fp32, self.total_tokens, c.n_q_heads, c.n_kv_heads,
+                                                c.head_dim, q, k, lse, out)
+        _check(rc, "cake_accumulate_attention")
+        return out
+
+    def attend_cache(self, layer: int, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                     row_offsets: torch.Tensor, *, k_tail: Optional[torch.Tensor] = None,
+                     v_tail: Optional[torch.Tensor] = None, tail_len: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                     ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Attention of one new token per request, q [n_req][H_q][d], over one layer of the packed cache that compact or
+        decode_begin returned, and over the first tail_len[r] rows of k_tail, v_tail [n_req][H_kv][capacity][d]:
+        (out, lse [n_req][H_q]).  Does not depend on the context's current batch."""
+        c = self.cfg
+        rc, out, lse = _fast.attend_cache(self._a, self._fp32, layer, c.n_layers, c.n_q_heads, c.n_kv_heads, c.head_dim, q,
+                                          row_offsets, k_tail, v_tail, tail_len, out, lse, k_cache, v_cache)
+        _check(rc, "cake_attend_cache")
+        return out, lse
+
+    def attend_int4(self, layer: int, q: torch.Tensor, cache: dict, *, k_tail: Optional[torch.Tensor] = None,
+                    v_tail: Optional[torch.Tensor] = None, tail_len: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """attend_cache over the dict of 4-bit rows that compact_int4 returned."""
+        c, x = self.cfg, cache
+        rc, out, lse = _fast.attend_int4(self._a, self._fp32, layer, c.n_layers, c.n_q_heads, c.n_kv_heads, c.head_dim, q,
+                                         x["row_offsets"], k_tail, v_tail, tail_len, out, lse, x["k_codes"], x["k_scale"],
+                                         x["k_zero"], x["v_codes"], x["v_scale"], x["v_zero"], x["kgroup_offsets"])
+        _check(rc, "cake_attend_int4")
+        return out, lse
 
     def set_wait_limit(self, cycles: int) -> None:
         _check(self.lib.cake_set_wait_limit(self._h, cycles), "cake_set_wait_limit")

@@ -10,8 +10,13 @@
 #include <dlfcn.h>
 
 #include <exception>
+#include <stdexcept>
+#include <string>
 #include <vector>
 
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -30,6 +35,11 @@ struct Lib {
   decltype(&cake_decode_step) decode_step;
   decltype(&cake_decode_get_state) decode_get_state;
   decltype(&cake_select_positions_static) select_positions_static;
+  decltype(&cake_attend_prompt) attend_prompt;
+  decltype(&cake_accumulate_attention) accumulate_attention;
+  decltype(&cake_attend_workspace_bytes) attend_workspace_bytes;
+  decltype(&cake_attend_cache) attend_cache;
+  decltype(&cake_attend_int4) attend_int4;
 } lib;
 
 // The current CUDA stream; false with a Python error set if there is none (no usable device).
@@ -170,6 +180,7 @@ PyObject* init(PyObject*, PyObject* path) {
   }
   SYM(begin) SYM(score_layer) SYM(allocate) SYM(evict) SYM(compact) SYM(compact_int4) SYM(clear_unused)
   SYM(decode_step) SYM(decode_get_state) SYM(select_positions_static)
+  SYM(attend_prompt) SYM(accumulate_attention) SYM(attend_workspace_bytes) SYM(attend_cache) SYM(attend_int4)
 #undef SYM
   Py_RETURN_NONE;
 }
@@ -337,10 +348,174 @@ PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n) {
   DONE(lib.select_positions_static((const float*)v, heads, len, keep, (int32_t*)o, st));
 }
 
+// ---- attention over prompts and caches: shapes are checked here, outputs allocated where none are given
+
+// The tensor of an argument, on the current device and of the wanted type and shape (-1: any size); `strided`: only its
+// channels have to be contiguous.  Throws what becomes a Python error.
+const at::Tensor& tensor(PyObject* o, const char* name, at::ScalarType want, at::IntArrayRef shape, bool strided = false) {
+  if (!THPVariable_Check(o)) throw std::invalid_argument(std::string(name) + ": expected a torch.Tensor");
+  const at::Tensor& t = THPVariable_Unpack(o);
+  auto fail = [&](const std::string& why) { throw std::invalid_argument(std::string(name) + ": " + why); };
+  if (!t.is_cuda()) fail("libcake takes CUDA tensors only");
+  if (t.get_device() != c10::cuda::current_device()) fail("tensor is not on the current device");
+  if (t.scalar_type() != want) fail(std::string("expected ") + c10::toString(want) + ", got " + c10::toString(t.scalar_type()));
+  bool same = t.dim() == (int64_t)shape.size();
+  for (size_t i = 0; same && i < shape.size(); ++i) same = shape[i] < 0 || t.size((int64_t)i) == shape[i];
+  if (!same) {
+    std::string w;
+    for (int64_t x : shape) w += (w.empty() ? "[" : ", ") + (x < 0 ? std::string("*") : std::to_string(x));
+    fail("expected shape " + w + "]");
+  }
+  if (strided ? t.size(-1) > 1 && t.stride(-1) != 1 : !t.is_contiguous()) fail("tensor must be contiguous");
+  return t;
+}
+at::Tensor tensor_or_new(PyObject* o, const char* name, at::ScalarType want, at::IntArrayRef shape, const at::Tensor& like) {
+  return o != Py_None ? tensor(o, name, want, shape) : at::empty(shape, like.options().dtype(want));
+}
+// Strides between heads and tokens of [head][token][channel]; what one head or token alone has is not its tensor's.
+void strides(const at::Tensor& t, int64_t& head, int64_t& token) {
+  token = t.size(1) > 1 ? t.stride(1) : t.size(2);
+  head = t.size(0) > 1 ? t.stride(0) : t.size(1) * token;
+}
+int64_t integer(PyObject* o) {
+  const int64_t v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw std::invalid_argument("");
+  return v;
+}
+template <typename F>
+PyObject* guarded(F f) {
+  try {
+    return f();
+  } catch (const std::invalid_argument& e) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+// (status, tensor or None, tensor or None)
+PyObject* answer(int32_t rc, const at::Tensor& a, const at::Tensor& b) {
+  PyObject* x = a.defined() ? THPVariable_Wrap(a) : Py_NewRef(Py_None);
+  PyObject* y = b.defined() ? THPVariable_Wrap(b) : Py_NewRef(Py_None);
+  return Py_BuildValue("iNN", (int)rc, x, y);
+}
+template <typename F>
+int32_t released(F f) {
+  void* st = (void*)c10::cuda::getCurrentCUDAStream().stream();
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f(st);
+  Py_END_ALLOW_THREADS
+  return rc;
+}
+
+// attend_prompt(ctx, is_fp32, n_req, tokens, q_heads, kv_heads, head_dim, window, q, k, v, out, lse, lse_window)
+PyObject* attend_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 14)) return nullptr;
+  return guarded([&] {
+    const at::ScalarType e = element(a[1]), f = at::ScalarType::Float;
+    const int64_t R = integer(a[2]), T = integer(a[3]), hq = integer(a[4]), hkv = integer(a[5]), d = integer(a[6]), w = integer(a[7]);
+    const at::Tensor &q = tensor(a[8], "q", e, {hq, T, d}, true), &k = tensor(a[9], "k", e, {hkv, T, d}),
+                     &v = tensor(a[10], "v", e, {hkv, T, d});
+    const at::Tensor out = a[11] != Py_None ? tensor(a[11], "out", e, {hq, T, d}, true) : at::empty_like(q);
+    const at::Tensor lse = tensor_or_new(a[12], "lse", f, {hq, T}, q);
+    float* lw = a[13] != Py_None ? (float*)tensor(a[13], "lse_window", f, {R, hq, w}).data_ptr() : nullptr;
+    int64_t qh, qt, oh, ot;
+    strides(q, qh, qt);
+    strides(out, oh, ot);
+    cake_ctx* c = ctx_of(a[0]);
+    const int32_t rc = released([&](void* st) {
+      return lib.attend_prompt(c, q.data_ptr(), qh, qt, k.data_ptr(), v.data_ptr(), out.data_ptr(), oh, ot, (float*)lse.data_ptr(),
+                               lw, st);
+    });
+    return answer(rc, out, lse);
+  });
+}
+
+// accumulate_attention(ctx, is_fp32, tokens, q_heads, kv_heads, head_dim, q, k, lse, out)
+PyObject* accumulate_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 10)) return nullptr;
+  return guarded([&] {
+    const at::ScalarType e = element(a[1]), f = at::ScalarType::Float;
+    const int64_t T = integer(a[2]), hq = integer(a[3]), hkv = integer(a[4]), d = integer(a[5]);
+    const at::Tensor &q = tensor(a[6], "q", e, {hq, T, d}, true), &k = tensor(a[7], "k", e, {hkv, T, d}),
+                     &lse = tensor(a[8], "lse", f, {hq, T});
+    const at::Tensor out = tensor_or_new(a[9], "out", f, {hkv, T}, q);
+    int64_t qh, qt;
+    strides(q, qh, qt);
+    cake_ctx* c = ctx_of(a[0]);
+    const int32_t rc = released([&](void* st) {
+      return lib.accumulate_attention(c, q.data_ptr(), qh, qt, k.data_ptr(), (const float*)lse.data_ptr(), (float*)out.data_ptr(), st);
+    });
+    return answer(rc, out, at::Tensor());
+  });
+}
+
+struct Tail {
+  const void *k = nullptr, *v = nullptr;
+  const int32_t* len = nullptr;
+  int64_t cap = 0;
+};
+Tail tail_of(PyObject* const* a, at::ScalarType e, int64_t n_req, int64_t hkv, int64_t d) {     // k_tail, v_tail, tail_len
+  Tail t;
+  if (a[0] == Py_None && a[1] == Py_None && a[2] == Py_None) return t;
+  const at::Tensor& k = tensor(a[0], "k_tail", e, {n_req, hkv, -1, d});
+  t.cap = k.size(2);
+  t.k = k.data_ptr();
+  t.v = tensor(a[1], "v_tail", e, {n_req, hkv, t.cap, d}).data_ptr();
+  t.len = (const int32_t*)tensor(a[2], "tail_len", at::ScalarType::Int, {n_req}).data_ptr();
+  return t;
+}
+
+// attend_cache(ctx, is_fp32, layer, n_layers, q_heads, kv_heads, head_dim, q, row_offsets, k_tail, v_tail, tail_len, out, lse,
+//              k_cache, v_cache)
+// attend_int4(the same up to lse, k_codes, k_scale, k_zero, v_codes, v_scale, v_zero, kgroup_offsets)
+PyObject* attend_cached(PyObject* const* a, bool int4) {
+  return guarded([&] {
+    const at::ScalarType e = element(a[1]), f = at::ScalarType::Float, u8 = at::ScalarType::Byte, i64 = at::ScalarType::Long;
+    const int64_t layer = integer(a[2]), L = integer(a[3]), hq = integer(a[4]), hkv = integer(a[5]), d = integer(a[6]);
+    const at::Tensor& q = tensor(a[7], "q", e, {-1, hq, d});
+    const int64_t R = q.size(0);
+    const int64_t* off = (const int64_t*)tensor(a[8], "row_offsets", i64, {R * L + 1}).data_ptr();
+    const Tail t = tail_of(a + 9, e, R, hkv, d);
+    if (R > INT32_MAX || layer != (int32_t)layer) throw std::invalid_argument("no such layer, or too many requests");
+    const at::Tensor out = a[12] != Py_None ? tensor(a[12], "out", e, {R, hq, d}) : at::empty_like(q);
+    const at::Tensor lse = tensor_or_new(a[13], "lse", f, {R, hq}, q);
+    cake_ctx* c = ctx_of(a[0]);
+    const int64_t bytes = lib.attend_workspace_bytes(c, (int32_t)R);
+    if (bytes < 0) return answer((int32_t)bytes, out, lse);
+    const at::Tensor ws = at::empty({bytes}, q.options().dtype(u8));
+    int32_t rc;
+    if (!int4) {
+      const at::Tensor &k = tensor(a[14], "k_cache", e, {-1, d}), &v = tensor(a[15], "v_cache", e, {-1, d});
+      rc = released([&](void* st) {
+        return lib.attend_cache(c, (int32_t)R, (int32_t)layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), off, t.k, t.v, t.len, t.cap,
+                                out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes, st);
+      });
+    } else {
+      const at::Tensor &kc = tensor(a[14], "k_codes", u8, {-1, d / 2}), &ks = tensor(a[15], "k_scale", f, {-1, d}),
+                       &kz = tensor(a[16], "k_zero", f, {ks.size(0), d}), &vc = tensor(a[17], "v_codes", u8, {kc.size(0), d / 2}),
+                       &vs = tensor(a[18], "v_scale", f, {kc.size(0), -1}), &vz = tensor(a[19], "v_zero", f, {kc.size(0), vs.size(1)});
+      const int64_t* koff = (const int64_t*)tensor(a[20], "kgroup_offsets", i64, {R * L + 1}).data_ptr();
+      if (vs.size(1) < 1 || d % vs.size(1)) throw std::invalid_argument("v_scale: no such group");
+      rc = released([&](void* st) {
+        return lib.attend_int4(c, (int32_t)R, (int32_t)layer, q.data_ptr(), (const uint8_t*)kc.data_ptr(), (const float*)ks.data_ptr(),
+                               (const float*)kz.data_ptr(), (const uint8_t*)vc.data_ptr(), (const float*)vs.data_ptr(),
+                               (const float*)vz.data_ptr(), (int32_t)(d / vs.size(1)), off, koff, t.k, t.v, t.len, t.cap,
+                               out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes, st);
+      });
+    }
+    return answer(rc, out, lse);
+  });
+}
+PyObject* attend_cache(PyObject*, PyObject* const* a, Py_ssize_t n) { return arity(n, 16) ? attend_cached(a, false) : nullptr; }
+PyObject* attend_int4(PyObject*, PyObject* const* a, Py_ssize_t n) { return arity(n, 21) ? attend_cached(a, true) : nullptr; }
+
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"init", init, METH_O, nullptr},
                          FAST(begin), FAST(score_layer), FAST(allocate), FAST(evict), FAST(prefill), FAST(compact),
                          FAST(compact_int4), FAST(clear_unused), FAST(decode_step), FAST(decode_get_state), FAST(select),
+                         FAST(attend_prompt), FAST(accumulate_attention), FAST(attend_cache), FAST(attend_int4),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cake_py", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
