@@ -39,6 +39,10 @@ struct Strided {
   int64_t head, token;
 };
 
+// attend_tc.cu
+bool prompt_tc_supported(const cake_ctx* ctx, Strided q);
+int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
+                         float* lse, float* lse_window, cudaStream_t st);
 // attend_simt.cu
 int32_t launch_prompt_simt(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
                            float* lse, float* lse_window, cudaStream_t st);

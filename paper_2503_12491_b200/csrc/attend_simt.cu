@@ -362,8 +362,9 @@ int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, 
   const bool by_token = out_head_stride >= d && out_token_stride >= d && out_token_stride - d >= (heads - 1) * out_head_stride;
   const bool by_head = out_token_stride >= d && out_head_stride >= d && out_head_stride - d >= (tokens - 1) * out_token_stride;
   if (!by_token && !(heads == 1 && out_token_stride >= d) && !by_head) return CAKE_ERR_ARG;
-  return launch_prompt_simt(ctx, q, {q_head_stride, q_token_stride}, k, v, out, {out_head_stride, out_token_stride}, lse,
-                            lse_window, (cudaStream_t)stream);
+  const Strided qs = {q_head_stride, q_token_stride}, os = {out_head_stride, out_token_stride};
+  return (prompt_tc_supported(ctx, qs) ? launch_prompt_tc : launch_prompt_simt)(ctx, q, qs, k, v, out, os, lse, lse_window,
+                                                                                (cudaStream_t)stream);
 }
 
 int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride, const void* k,

@@ -1,0 +1,542 @@
+// Attention over whole prompts on the sm_100a tensor cores: bf16 inputs, causal, grouped heads, packed requests.
+//
+//   prompt_tc   O_i = sum_{j<=i} softmax_j(q_i.k_j / sqrt d) v_j and lse_i = log sum_{j<=i} exp(q_i.k_j / sqrt d).
+//
+// A CTA works for 256 consecutive rows of one query head, as two tiles A and B of 128 rows, and goes over its key tiles of 128
+// keys once, in ascending order:
+//     S = Q K^T  (tcgen05, accumulator in tensor memory)  ->  P = 2^(s - ref), in bf16, back into tensor memory over S
+//     O += P V   (tcgen05, P read from tensor memory, V as it lies in HBM: keys x channels)
+// A thread of a softmax group owns one row: its logits come with tcgen05.ld, so a row's maximum and sum need no other
+// thread.  While group A works on its logits, the tensor cores multiply for group B and the other way round.
+//
+// Reference.  P is taken against a reference that follows the row's running maximum only when that is more than 2^8 above
+// it (the output would have to be rescaled in tensor memory for every new maximum): sums are exact in the reference, which
+// cancels in O / sum and is added back in the log-sum-exp.
+//
+// Bound.  A tile pair is 2 x 128 x 128 logits: 2 x 2 products of 512 cycles at d = 128 on the tensor cores, and 32 768
+// exponentials, 2048 cycles of the special-function unit; a share of the exponentials is computed by a polynomial on the
+// FMA pipe (exp2_poly), so that the tensor cores set the pace.
+//
+// Rounding.  P is rounded to bf16 as the operand of a bf16 product; its sum is taken before the rounding, in fp32; logits,
+// sums and outputs are fp32.
+//
+// Warps: 0-3 softmax of tile A, 4-7 of tile B, 8 TMA loads, 9 MMAs and tensor-memory allocation, 10-11 look through the value
+// tiles on the diagonal: a value that some row of the tile must not see is multiplied by a weight of zero, which only helps
+// if it is finite, so those that are not are zeroed here and added to the rows that do see them at the end.
+// Every wait is bounded; one that runs out raises CAKE_ERR_TIMEOUT and the CTA drains and exits.
+#include "attend.cuh"
+#include "tc_ptx.cuh"
+
+#include <algorithm>
+
+namespace cake {
+namespace {
+
+constexpr int TILE = 128;
+constexpr int SLAB = TILE * 128;                 // bytes of 64 channels of a tile of 128 rows
+constexpr int P_THREADS = 384;
+constexpr int W_TMA = 8, W_MMA = 9, W_SCAN = 10;
+constexpr float kRefSlack = 8.f;                 // powers of two that a row's maximum may lie above its reference
+
+template <int D> struct PromptCfg {
+  static constexpr int SLABS = D / 64;
+  static constexpr int TILE_BYTES = SLABS * SLAB;
+  static constexpr int STAGES = D == 128 ? 4 : 6;                    // K and V tiles in flight
+  static constexpr size_t SMEM = 1024 + (size_t)(2 + STAGES) * TILE_BYTES + 256;
+  static constexpr uint32_t O_COL = 256;                             // tensor memory: S/P of A, of B, O of A, of B
+};
+static_assert(PromptCfg<128>::SMEM <= 227 * 1024 && PromptCfg<64>::SMEM <= 227 * 1024, "a CTA has 227 KB of shared memory");
+
+struct PromptParams {
+  const __nv_bfloat16* v;                        // for the rows of the fix-up alone
+  __nv_bfloat16* out;
+  float *lse, *lse_window;
+  Strided os;
+  int64_t T;
+  int32_t* status;
+  long long limit;
+  int Hq, G, window;
+  int q_head_step, q_token_step;                 // 0 where all heads (tokens) are the same row in memory
+  float scale, scale2;
+};
+
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2) {
+  asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
+               "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n}"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+// D = A B + (kAcc ? D : 0) with A in tensor memory (16 bf16 of K per step: 8 columns) and B in shared memory, K rows of 64
+// channels in the 128-byte swizzle: the operand's N runs along the row, and beyond 64 channels in the next slab
+// (leading-dimension offset); 8 rows of K are 1024 bytes (stride offset).
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\nmov.b64 db, {%2, %5};\n"
+               "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}"
+               ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi) : "memory");
+}
+#define R32(r) "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), \
+  "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), \
+  "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+#define L32 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, " \
+  "%28, %29, %30, %31}"
+// 32 fp32 columns of this thread's TMEM lane (valid after tmem_wait_ld, which must come before any use).
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " L32 ", [%32];" : R32(r) : "r"(addr));
+}
+#define RW32(r) "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), \
+  "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), \
+  "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+// The registers pass through the statement, so that none of their uses is scheduled before it.
+__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) { asm volatile("tcgen05.wait::ld.sync.aligned;" : RW32(r) : : "memory"); }
+__device__ __forceinline__ void pin32(uint32_t* r) { asm volatile("" : RW32(r)); }
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+               "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+               "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+               "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// 2^x of two values on the FMA pipe, x <= 100: x = n + f with n an integer and |f| <= 1/2, 2^f by its minimax polynomial of
+// degree 5 (7.5e-8 relative, a Remez fit), times 2^n put together from its bits: zero from n = -127 down.  A NaN stays one.
+__device__ __forceinline__ f32x2 splat(float x) { return pack2(x, x); }
+__device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
+  float x0, x1;
+  unpack2(x, x0, x1);
+  x = pack2(max_or_nan(x0, -127.f), max_or_nan(x1, -127.f));
+  const f32x2 r = add2(x, splat(12582912.f));                     // 1.5 * 2^23: the integer lands in the low bits
+  const f32x2 f = fma2(add2(r, splat(-12582912.f)), splat(-1.f), x);
+  f32x2 p = fma2(f, splat(1.3276472454890609e-3f), splat(9.675540961325169e-3f));
+  p = fma2(p, f, splat(5.550713092088699e-2f));
+  p = fma2(p, f, splat(2.4022120237350464e-1f));
+  p = fma2(p, f, splat(6.931469440460205e-1f));
+  p = fma2(p, f, splat(1.0000001192092896f));
+  float r0, r1;
+  unpack2(r, r0, r1);
+  unpack2(mul2(p, pack2(__uint_as_float((__float_as_uint(r0) << 23) + 0x3F800000u),
+                        __uint_as_float((__float_as_uint(r1) << 23) + 0x3F800000u))), a, b);
+}
+
+// ------------------------------------------------------------------ prompt
+struct PromptSmem {
+  uint8_t *q, *kv;
+  uint64_t *q_full, *kv_full, *kv_empty, *s_full, *p_full, *o_full, *vd_full, *v_clean, *drained;
+  uint32_t* tmem;
+  int* dirty;                                    // [2] a value tile on the diagonal of A, of B had values that are not finite
+};
+
+template <int D>
+__device__ __forceinline__ PromptSmem carve(uint8_t* base) {
+  using C = PromptCfg<D>;
+  PromptSmem s;
+  uint8_t* p = (uint8_t*)(((uintptr_t)base + 1023) & ~(uintptr_t)1023);
+  s.q = p;                      p += 2 * C::TILE_BYTES;
+  s.kv = p;                     p += C::STAGES * C::TILE_BYTES;
+  s.q_full = (uint64_t*)p;      p += 8;
+  s.kv_full = (uint64_t*)p;     p += 8 * C::STAGES;
+  s.kv_empty = (uint64_t*)p;    p += 8 * C::STAGES;
+  s.s_full = (uint64_t*)p;      p += 16;
+  s.p_full = (uint64_t*)p;      p += 32;         // [tile][half]
+  s.o_full = (uint64_t*)p;      p += 16;
+  s.vd_full = (uint64_t*)p;     p += 16;
+  s.v_clean = (uint64_t*)p;     p += 16;
+  s.drained = (uint64_t*)p;     p += 8;
+  s.tmem = (uint32_t*)p;        p += 8;
+  s.dirty = (int*)p;
+  return s;
+}
+
+// One row's tile of logits: reference, exponentials, P into tensor memory.  kDiag: keys behind the row are masked.
+template <int D, bool kDiag>
+__device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, bool first, int row, float scale2, float& ref, float& sum,
+                                             uint64_t* p_full) {
+  uint32_t r[128];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, r + 32 * c);
+  tmem_wait_ld32(r);
+  pin32(r + 32); pin32(r + 64); pin32(r + 96);
+  float* s = reinterpret_cast<float*>(r);
+  if constexpr (kDiag) {
+#pragma unroll
+    for (int c = 0; c < 128; ++c) s[c] = c > row ? -CUDART_INF_F : s[c];
+  }
+  float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
+#pragma unroll
+  for (int c = 4; c < 128; c += 8) {
+    m0 = max3(m0, s[c], s[c + 1]);
+    m1 = max3(m1, s[c + 2], s[c + 3]);
+    if (c + 4 < 128) {
+      m2 = max3(m2, s[c + 4], s[c + 5]);
+      m3 = max3(m3, s[c + 6], s[c + 7]);
+    }
+  }
+  const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale2;
+  if (first) {
+    ref = top;
+  } else if (__any_sync(0xffffffffu, top > ref + kRefSlack)) {
+    // Some row's maximum left its reference behind: the warp's outputs move to the new ones.  (The products of the tile
+    // before are done: this tile's logits were committed after them.)
+    const float to = top > ref + kRefSlack ? top : ref, f = to == ref ? 1.f : ex2(ref - to);
+    sum *= f;
+    ref = to;
+    uint32_t o[32];
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+      tmem_ld32(t_o + c, o);
+      tmem_wait_ld32(o);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+      tmem_st32(t_o + c, o);
+    }
+  }
+  const f32x2 sc = splat(scale2), mr = splat(-ref);
+  f32x2 acc0 = splat(0.f), acc1 = splat(0.f);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    uint32_t p[32];
+#pragma unroll
+    for (int c = 0; c < 64; c += 8) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const f32x2 x = fma2(pack2(s[64 * half + c + i], s[64 * half + c + i + 1]), sc, mr);
+        if (!kDiag && i == 6) {                  // a quarter of the exponentials on the FMA pipe
+          exp2_poly(x, e[i], e[i + 1]);
+        } else {
+          float a, b;
+          unpack2(x, a, b);
+          e[i] = ex2(a);
+          e[i + 1] = ex2(b);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const __nv_bfloat162 w = __floats2bfloat162_rn(e[i], e[i + 1]);
+        p[(c + i) / 2] = *reinterpret_cast<const uint32_t*>(&w);
+      }
+      acc0 = add2(acc0, pack2(e[0], e[1]));
+      acc1 = add2(acc1, pack2(e[2], e[3]));
+      acc0 = add2(acc0, pack2(e[4], e[5]));
+      acc1 = add2(acc1, pack2(e[6], e[7]));
+    }
+    tmem_st32(t_s + 32 * half, p);
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&p_full[half]);
+  }
+  float a, b, c, d;
+  unpack2(acc0, a, b);
+  unpack2(acc1, c, d);
+  sum += (a + b) + (c + d);
+}
+
+template <int D>
+__global__ void __launch_bounds__(P_THREADS, 1)
+prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+          const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptBatch B, const PromptParams P) {
+  using C = PromptCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const PromptSmem S = carve<D>(smem_raw);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int tile = blockIdx.x / P.Hq, h = blockIdx.x % P.Hq, g = h / P.G;
+  const int r = request_of(B, tile), N = B.len[r];
+  const int row0 = (B.first[r + 1] - 1 - tile) * 2 * TILE;           // the last rows have the most keys: they come first
+  const int64_t cu = B.cu[r];
+  const int n_a = row0 / TILE + 1, n_b = row0 + TILE < N ? n_a + 1 : 0, n_kv = max(n_a, n_b);   // key tiles of A, of B
+
+  if (threadIdx.x == 0) {
+    mbar_init(S.q_full, 1);
+    for (int i = 0; i < C::STAGES; ++i) { mbar_init(&S.kv_full[i], 1); mbar_init(&S.kv_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&S.s_full[i], 1); mbar_init(&S.o_full[i], 1); mbar_init(&S.vd_full[i], 1); mbar_init(&S.v_clean[i], 2); S.dirty[i] = 0; }
+    for (int i = 0; i < 4; ++i) mbar_init(&S.p_full[i], 4);
+    mbar_init(S.drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == W_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(S.tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *S.tmem;
+  // Item i of the ring: K of tile 0, then V of tile j and K of tile j + 1 in turn.
+  const int n_items = 2 * n_kv;
+  auto stage_of = [](int i) { return i % C::STAGES; };
+  auto phase_of = [](int i) { return (uint32_t)(i / C::STAGES) & 1u; };
+  auto k_item = [](int j) { return j == 0 ? 0 : 2 * j; };
+  auto v_item = [](int j) { return 2 * j + 1; };
+  // The value tiles on the diagonals of A and B, the last ones, arrive at barriers of their own, where the scan waits.  (Their
+  // stages are not used again: at most two items come behind them.)
+  static_assert(C::STAGES > 2, "");
+  auto diag_of = [&](int i) { return (i & 1) == 0 ? -1 : i == v_item(n_a - 1) ? 0 : i == v_item(n_b - 1) ? 1 : -1; };
+  auto full_of = [&](int i) { return diag_of(i) < 0 ? &S.kv_full[stage_of(i)] : &S.vd_full[diag_of(i)]; };
+
+  if (warp == W_TMA) {
+    mbar_expect_tx(S.q_full, (uint32_t)((n_b ? 2 : 1) * C::TILE_BYTES));
+    for (int t = 0; t < (n_b ? 2 : 1); ++t)
+      for (int sl = 0; sl < C::SLABS; ++sl)
+        tma_load_4d(S.q + t * C::TILE_BYTES + sl * SLAB, &q_map, S.q_full, 64 * sl,
+                    (int)(cu + row0 + t * TILE) * P.q_token_step, h * P.q_head_step, 0);
+    bool ok = true;
+    int issued = 0;
+    for (int i = 0; i < n_items; ++i) {
+      ok = mbar_wait(&S.kv_empty[stage_of(i)], phase_of(i) ^ 1u, P.status, P.limit);
+      if (!ok) break;
+      const bool is_v = i & 1;
+      const int j = i >> 1;
+      mbar_expect_tx(full_of(i), C::TILE_BYTES);
+      tma_load_3d(S.kv + stage_of(i) * C::TILE_BYTES, is_v ? &v_map : &k_map, full_of(i), 0, (int)(g * P.T + cu) + j * TILE, 0);
+      issued = i + 1;
+    }
+    // do not leave the CTA while a copy may still be writing its shared memory
+    mbar_wait(S.q_full, 0, P.status, P.limit);
+    for (int i = max(0, issued - C::STAGES); i < issued; ++i)
+      mbar_wait(full_of(i), diag_of(i) < 0 ? phase_of(i) : 0u, P.status, P.limit);
+  } else if (warp == W_MMA) {
+    const uint32_t id_s = instr_desc(TILE, TILE), id_o = instr_desc(TILE, D) | (1u << 16);   // B of the second: N along the row
+    const uint32_t q_lo = (smem_u32(S.q) & 0x3FFFFu) >> 4, kv_lo = (smem_u32(S.kv) & 0x3FFFFu) >> 4;
+    bool ok = mbar_wait(S.q_full, 0, P.status, P.limit);
+    auto qk = [&](int t, int j) {                // S_t = Q_t K_j^T
+      const uint32_t a = q_lo + (uint32_t)(t * C::TILE_BYTES >> 4), b = kv_lo + (uint32_t)(stage_of(k_item(j)) * C::TILE_BYTES >> 4);
+      const uint32_t d = tmem + 128u * t;
+      umma_ss<0>(d, a, b, id_s);
+      umma_ss<1>(d, a + 2, b + 2, id_s);
+      umma_ss<1>(d, a + 4, b + 4, id_s);
+      umma_ss<1>(d, a + 6, b + 6, id_s);
+      if constexpr (D == 128) {
+        constexpr uint32_t o = SLAB >> 4;
+        umma_ss<1>(d, a + o, b + o, id_s);
+        umma_ss<1>(d, a + o + 2, b + o + 2, id_s);
+        umma_ss<1>(d, a + o + 4, b + o + 4, id_s);
+        umma_ss<1>(d, a + o + 6, b + o + 6, id_s);
+      }
+      umma_commit(&S.s_full[t]);
+    };
+    auto pv = [&](int t, int j) {                // O_t += P_t V_j, half of the keys as soon as its weights are there
+      const uint32_t b = (kv_lo + (uint32_t)(stage_of(v_item(j)) * C::TILE_BYTES >> 4)) | ((uint32_t)(SLAB >> 4) << 16);
+      const uint32_t d = tmem + C::O_COL + (uint32_t)(D * t), a = tmem + 128u * t;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (!mbar_wait(&S.p_full[2 * t + half], (uint32_t)j & 1u, P.status, P.limit)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
+          umma_ts(d, a + 8 * ks, b + (uint32_t)(ks * 2048 >> 4), id_o, (uint32_t)(j > 0 || ks > 0));
+      }
+      return true;
+    };
+    if (ok) ok = mbar_wait(&S.kv_full[0], 0, P.status, P.limit);
+    if (ok) {
+      tc_fence_after();
+      qk(0, 0);
+      if (n_b) qk(1, 0);
+      umma_commit(&S.kv_empty[0]);
+    }
+    for (int j = 0; ok && j < n_kv; ++j) {
+      const int vi = v_item(j), ki = k_item(j + 1);
+      const int diag = diag_of(vi);
+      ok = mbar_wait(diag >= 0 ? &S.v_clean[diag] : &S.kv_full[stage_of(vi)], diag >= 0 ? 0u : phase_of(vi), P.status, P.limit);
+      if (!ok) break;
+      if (j < n_a) {
+        ok = pv(0, j);
+        if (!ok) break;
+        if (j == n_a - 1) umma_commit(&S.o_full[0]);
+      }
+      if (j + 1 < n_kv) {
+        ok = mbar_wait(&S.kv_full[stage_of(ki)], phase_of(ki), P.status, P.limit);
+        if (!ok) break;
+        tc_fence_after();
+        if (j + 1 < n_a) qk(0, j + 1);
+      }
+      if (j < n_b) {
+        ok = pv(1, j);
+        if (!ok) break;
+        if (j == n_b - 1) umma_commit(&S.o_full[1]);
+      }
+      umma_commit(&S.kv_empty[stage_of(vi)]);
+      if (j + 1 < n_kv) {
+        if (j + 1 < n_b) qk(1, j + 1);
+        umma_commit(&S.kv_empty[stage_of(ki)]);
+      }
+    }
+    if (!ok) {                                   // what was issued ends before tensor and shared memory are given back
+      umma_commit(S.drained);
+      mbar_wait(S.drained, 0, P.status, P.limit);
+    }
+  } else if (warp >= W_SCAN) {
+    // the value tiles on the diagonals: j = n_a - 1 and n_b - 1
+    for (int t = 0; t < (n_b ? 2 : 1); ++t) {
+      const int vi = v_item(t ? n_b - 1 : n_a - 1);
+      if (!mbar_wait(&S.vd_full[t], 0, P.status, P.limit)) break;
+      uint4* x = reinterpret_cast<uint4*>(S.kv + stage_of(vi) * C::TILE_BYTES);
+      bool found = false;
+#pragma unroll 4
+      for (int i = threadIdx.x - W_SCAN * 32; i < C::TILE_BYTES / 16; i += 64) {
+        uint4 v = x[i];
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
+        if (bad) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+            if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0x0000FFFFu;
+          }
+          x[i] = v;
+          found = true;
+        }
+      }
+      if (found) S.dirty[t] = 1;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.v_clean[t]);
+    }
+  } else {
+    const int t = warp >> 2, n = t ? n_b : n_a, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + 128u * t, t_o = tmem + lanes + C::O_COL + (uint32_t)(D * t);
+    float ref = 0.f, sum = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n - 1 && ok; ++j) {
+      ok = mbar_wait(&S.s_full[t], (uint32_t)j & 1u, P.status, P.limit);
+      if (!ok) break;
+      tc_fence_after();
+      softmax_tile<D, false>(t_s, t_o, j == 0, row, P.scale2, ref, sum, S.p_full + 2 * t);
+    }
+    if (ok && n) {
+      ok = mbar_wait(&S.s_full[t], (uint32_t)(n - 1) & 1u, P.status, P.limit);
+      if (ok) {
+        tc_fence_after();
+        softmax_tile<D, true>(t_s, t_o, n == 1, row, P.scale2, ref, sum, S.p_full + 2 * t);
+        ok = mbar_wait(&S.o_full[t], 0, P.status, P.limit);
+      }
+    }
+    if (ok && n) {
+      tc_fence_after();
+      const int i = row0 + t * TILE + row;       // the row in its request
+      const float inv = 1.f / sum;
+      const bool live = i < N;
+      __nv_bfloat16* dst = P.out + h * P.os.head + (cu + i) * P.os.token;
+      const __nv_bfloat16* vals = P.v + (g * P.T + cu) * D;
+      const int dirty = S.dirty[0] | (t ? S.dirty[1] << 1 : 0);      // (a row of A sees nothing of B's diagonal tile)
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        tmem_ld32(t_o + c, o);
+        tmem_wait_ld32(o);
+        float x[32];
+#pragma unroll
+        for (int u = 0; u < 32; ++u) x[u] = __uint_as_float(o[u]) * inv;
+        if (dirty && live) {
+          // values that are not finite and that this row sees: they decide its output, whatever their weight
+          for (int j = (n_a - 1) * TILE; j <= i; ++j)
+#pragma unroll
+            for (int u = 0; u < 32; ++u) {
+              const float w = __bfloat162float(vals[(int64_t)j * D + c + u]);
+              if (!isfinite(w)) x[u] += w;
+            }
+        }
+        if (live) {
+#pragma unroll
+          for (int u = 0; u < 32; u += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __nv_bfloat162 y = __floats2bfloat162_rn(x[u + 2 * e], x[u + 2 * e + 1]);
+              w[e] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            *reinterpret_cast<uint4*>(dst + c + u) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (live) {
+        const float l = (ref + log2f(sum)) * kLn2;
+        if (P.lse) P.lse[h * P.T + cu + i] = l;
+        const int w = i - (N - P.window);
+        if (P.lse_window && w >= 0) P.lse_window[((int64_t)B.req[r] * P.Hq + h) * P.window + w] = l;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == W_MMA) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host
+bool encode(CUtensorMap* map, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  const EncodeTiledFn enc = encode_fn();
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(p), dims, strides, box, es,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// K or V [rows][d] as (64 channels, rows, slabs): a box is a tile, slab by slab
+bool encode_rows(CUtensorMap* map, const void* p, int64_t rows, int d) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(d / 64)}, strides[2] = {(cuuint64_t)d * 2, 128};
+  const cuuint32_t box[3] = {64, TILE, (cuuint32_t)(d / 64)};
+  return encode(map, p, 3, dims, strides, box);
+}
+// Queries as (channels, tokens, heads, 1); an axis whose rows are one row in memory has one entry
+bool encode_q(CUtensorMap* map, const void* p, const cake_ctx* ctx, Strided s) {
+  const cake_config& c = ctx->cfg;
+  const cuuint64_t any = 16;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, s.token ? (cuuint64_t)ctx->total_tokens : 1,
+                              s.head ? (cuuint64_t)c.n_q_heads : 1, 1};
+  const cuuint64_t strides[3] = {s.token ? (cuuint64_t)s.token * 2 : any, s.head ? (cuuint64_t)s.head * 2 : any, any};
+  const cuuint32_t box[4] = {64, TILE, 1, 1};
+  return encode(map, p, 4, dims, strides, box);
+}
+
+}  // namespace
+
+bool prompt_tc_supported(const cake_ctx* ctx, Strided q) {
+  // (all tokens in one row: a box of 128 tokens does not fit such an axis)
+  return ctx->cfg.dtype == CAKE_DTYPE_BF16 && (int64_t)ctx->cfg.n_kv_heads * ctx->total_tokens < ((int64_t)1 << 31) && q.token != 0;
+}
+
+template <int D>
+static cudaError_t run_prompt_tc(const cake_ctx* ctx, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm,
+                                 const PromptBatch& B, const PromptParams& P, cudaStream_t st) {
+  static PerDeviceOnce once;
+  if (once.need(ctx->device)) {
+    const cudaError_t e = cudaFuncSetAttribute(prompt_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PromptCfg<D>::SMEM);
+    if (e != cudaSuccess) return e;
+    once.mark(ctx->device);
+  }
+  prompt_tc<D><<<(unsigned)(B.tiles * P.Hq), P_THREADS, PromptCfg<D>::SMEM, st>>>(qm, km, vm, B, P);
+  count_launch();
+  return cudaGetLastError();
+}
+
+int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
+                         float* lse, float* lse_window, cudaStream_t st) {
+  const cake_config& c = ctx->cfg;
+  CUtensorMap qm, km, vm;
+  const int64_t rows = c.n_kv_heads * ctx->total_tokens;
+  if (!encode_q(&qm, q, ctx, qs) || !encode_rows(&km, k, rows, c.head_dim) || !encode_rows(&vm, v, rows, c.head_dim))
+    return CAKE_ERR_CUDA;
+  PromptParams P;
+  P.v = (const __nv_bfloat16*)v; P.out = (__nv_bfloat16*)out; P.lse = lse; P.lse_window = lse_window; P.os = os;
+  P.T = ctx->total_tokens; P.status = ctx->d_status;
+  P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
+  P.Hq = c.n_q_heads; P.G = c.n_q_heads / c.n_kv_heads; P.window = c.window;
+  P.q_head_step = qs.head != 0; P.q_token_step = qs.token != 0;
+  P.scale = 1.f / sqrtf((float)c.head_dim);
+  P.scale2 = kLog2E / sqrtf((float)c.head_dim);
+  PromptBatch B;
+  for (int lo = 0; lo < ctx->n_req; lo += B.n) {
+    fill_prompt_batch(ctx, lo, 2 * TILE, B);
+    CAKE_CUDA_TRY(c.head_dim == 128 ? run_prompt_tc<128>(ctx, qm, km, vm, B, P, st) : run_prompt_tc<64>(ctx, qm, km, vm, B, P, st));
+  }
+  return CAKE_OK;
+}
+
+}  // namespace cake

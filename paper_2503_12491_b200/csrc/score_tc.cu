@@ -40,9 +40,8 @@
 // warp 14 merges rows, warp 15 stages the denominators of the next pass-B op in shared memory.  Every wait
 // (mbarrier or exchanged row) is bounded; a timed-out wait raises CAKE_ERR_TIMEOUT and the CTA
 // drains and exits.
-#include "cake_internal.cuh"
+#include "tc_ptx.cuh"
 
-#include <cuda.h>
 #include <math_constants.h>
 
 #include <algorithm>
@@ -64,7 +63,6 @@ constexpr int WARP_TMA = NWG * 4, WARP_MMA = NWG * 4 + 1, WARP_MERGE = NWG * 4 +
               WARP_LSE = NWG * 4 + 3;
 constexpr int NSTATW = NWG * 4;      // statistics warps
 constexpr int SLAB_BYTES = TILE * 128;   // one 64-element slab of a 128-row tile
-constexpr long long kSpinLimit = 4000000000ll;   // default cycles (~2 s) before a wait gives up
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kTileSumMax = 1.2676506e30f;    // pass A: a tile whose sum is beyond 2^100 is taken again from its maxima,
 constexpr float kShiftSum = 256.f;              // one beyond this moves the row's reference up afterwards
@@ -97,117 +95,6 @@ struct TcParams {
   int reps;                     // copies of the window rows in a pass-A tile: 128 / rows for 32 and 64 rows, else 1
 };
 
-// ------------------------------------------------------------------ PTX
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
-  asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-               "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(smem_u32(bar)),
-               "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n.reg .pred p;\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      "selp.b32 %0, 1, 0, p;\n}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait of a whole warp: false (and the sticky status set) if the phase never completes.  Its lanes agree: what
-// follows (TMEM loads, votes, elected issue) is the whole warp's, and a phase may complete just as the limit is reached.
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int32_t* status,
-                                          long long limit) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  const long long t0 = clock64();
-  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
-    if (__any_sync(0xffffffffu, clock64() - t0 > limit)) {
-      atomicCAS(status, 0, CAKE_ERR_TIMEOUT);
-      return false;
-    }
-  }
-  return true;
-}
-// 3-D tiled TMA load with an L2 eviction-priority hint: a whole key tile (both 64-element slabs)
-// in one copy.
-__device__ __forceinline__ void tma_load_3d_hint(void* dst, const CUtensorMap* map, uint64_t* bar,
-                                                 int c0, int c1, int c2, uint64_t policy) {
-  asm volatile(
-      "{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-      "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
-      "[%0], [%1, {%3, %4, %5}], [%2], %6;\n}"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
-  asm volatile(
-      "{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-      "@e cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];\n}"
-      ::"l"(map), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
-__device__ __forceinline__ uint64_t l2_policy_evict_last() {
-  uint64_t p;
-  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
-  return p;
-}
-__device__ __forceinline__ uint64_t l2_policy_evict_first() {
-  uint64_t p;
-  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-  return p;
-}
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
-                                            int c1, int c2, int c3) {
-  asm volatile(
-      "{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-      "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n}"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-      : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() {
-  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_after() {
-  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-// The MMA and TMA warps run converged, all 32 lanes executing the same loop, and one elected lane
-// issues each asynchronous instruction.  Issued from inside a one-lane branch the operands of
-// every tcgen05.mma are moved to uniform registers one by one and an M128 x N128 x K16 MMA costs
-// about 70 cycles to issue, more than the 64 cycles it takes to execute; from a converged warp
-// the descriptor arithmetic stays in the uniform datapath and the tensor pipe sets the pace.
-// Descriptors differ only in the 14-bit address field of their low word, the high word (stride,
-// version, swizzle) is a constant, and the accumulate flag is an immediate.
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // SBO, version 1, SWIZZLE_128B
-template <int kAcc>
-__device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
-  asm volatile(
-      "{\n.reg .pred p, e;\n.reg .b64 da, db;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\n"
-      "mov.b64 da, {%1, %5};\nmov.b64 db, {%2, %5};\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}"
-      ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAcc), "r"(kDescHi)
-      : "memory");
-}
-// The same with an explicit high descriptor word: operands that are not in the 128-byte swizzle.
-template <int kAcc>
-__device__ __forceinline__ void umma_ss_hi(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
-                                           uint32_t hi) {
-  asm volatile(
-      "{\n.reg .pred p, e;\n.reg .b64 da, db;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\n"
-      "mov.b64 da, {%1, %5};\nmov.b64 db, {%2, %5};\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}"
-      ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAcc), "r"(hi)
-      : "memory");
-}
 // Pass B folds the rows' log-sum-exps into the contraction: one more K = 16 step whose key-side
 // operand holds 1 in its first three columns and whose row-side operand holds -lse / scale split
 // into three bf16 terms, so the accumulator is (q.k - lse/scale) and the statistics warps neither
@@ -218,91 +105,6 @@ constexpr uint32_t kExtBytes = 128 * 32;
 constexpr uint32_t kExtDescHi = (256u >> 4) | (1u << 14);            // SBO, version 1, no swizzle
 constexpr uint32_t kExtDescLoLbo = (128u >> 4) << 16;                // LBO field of the low word
 __device__ __forceinline__ uint32_t ext_row_offset(int r) { return (uint32_t)((r >> 3) * 256 + (r & 7) * 16); }
-
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-               "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
-               ::"r"(smem_u32(bar)) : "memory");
-}
-// Starts the load of 16 consecutive fp32 columns of this thread's TMEM lane; the registers
-// are valid only after tmem_ld_wait on the same array.
-__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-// Waits for the thread's outstanding TMEM loads.  The registers pass through the statement so
-// that no use of them can be scheduled before it.
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-// Columns [lo, hi) of this thread's TMEM lane, 16 at a time: f(chunk) while the next chunk is on its way, so
-// that a warp has exponentials to issue all the time; `loaded` is called once all columns are in registers.
-template <typename F, typename L>
-__device__ __forceinline__ void for_columns(uint32_t taddr, int lo, int hi, F f, L loaded) {
-  uint32_t r0[16], r1[16];
-  tmem_ld16_issue(taddr + lo, r0);
-#pragma unroll 1
-  for (int c = lo; c < hi; c += 32) {
-    tmem_ld_wait(r0);
-    if (c + 16 < hi) tmem_ld16_issue(taddr + c + 16, r1);
-    else loaded();
-    f(r0);
-    if (c + 16 >= hi) break;
-    tmem_ld_wait(r1);
-    if (c + 32 < hi) tmem_ld16_issue(taddr + c + 32, r0);
-    else loaded();
-    f(r1);
-  }
-}
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Two fp32 values in one 64-bit register and the packed fp32x2 arithmetic on them: one
-// instruction issue for two FMAs or adds.  The statistics loops are bound by issue slots, not by
-// the FMA pipe, so halving their FFMA/FADD count matters although the pipe rate is the same.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
-  f32x2 v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-  return v;
-}
-__device__ __forceinline__ void unpack2(f32x2 v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-// Instruction descriptor: bf16 x bf16 -> fp32, both operands K-major, M x N tile.
-__device__ __forceinline__ uint32_t instr_desc(int M, int N) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
 
 // Rows that CTAs exchange carry the mark of the launch that wrote them, in the same 16 (or 8) bytes as the
 // data: they are written and read as one access each, so a reader that sees the mark has the data, and
@@ -1068,26 +870,6 @@ score_fused_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                  : "memory");
   }
 }
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)p;
-  }
-  return fn;
-}
-
 
 template <int G>
 cudaError_t launch_g(int device, bool entropy_b, bool copies, bool direct, bool early, int n_cta, cudaStream_t st, const CUtensorMap& qmap,
