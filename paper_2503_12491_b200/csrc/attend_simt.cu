@@ -373,7 +373,8 @@ int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_s
   if (ok != CAKE_OK || ctx->n_req == 0) return ok;
   if (!q || !k || !lse || !out) return CAKE_ERR_ARG;
   if (!rows_ok(ctx, q, q_head_stride, q_token_stride) || !rows_ok(ctx, k, 0, 0)) return CAKE_ERR_ARG;
-  return launch_accumulate_simt(ctx, q, {q_head_stride, q_token_stride}, k, lse, out, (cudaStream_t)stream);
+  const Strided qs = {q_head_stride, q_token_stride};
+  return (prompt_tc_supported(ctx, qs) ? launch_accumulate_tc : launch_accumulate_simt)(ctx, q, qs, k, lse, out, (cudaStream_t)stream);
 }
 
 }  // extern "C"

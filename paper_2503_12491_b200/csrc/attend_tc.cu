@@ -1,8 +1,9 @@
 // Attention over whole prompts on the sm_100a tensor cores: bf16 inputs, causal, grouped heads, packed requests.
 //
-//   prompt_tc   O_i = sum_{j<=i} softmax_j(q_i.k_j / sqrt d) v_j and lse_i = log sum_{j<=i} exp(q_i.k_j / sqrt d).
+//   prompt_tc       O_i = sum_{j<=i} softmax_j(q_i.k_j / sqrt d) v_j and lse_i = log sum_{j<=i} exp(q_i.k_j / sqrt d).
+//   accumulate_tc   A_j = 1/G sum_h sum_{i>=j} exp(q_hi.k_j / sqrt d - lse_hi): see there.
 //
-// A CTA works for 256 consecutive rows of one query head, as two tiles A and B of 128 rows, and goes over its key tiles of 128
+// prompt_tc.  A CTA works for 256 consecutive rows of one query head, as two tiles A and B of 128 rows, and goes over its key tiles of 128
 // keys once, in ascending order:
 //     S = Q K^T  (tcgen05, accumulator in tensor memory)  ->  P = 2^(s - ref), in bf16, back into tensor memory over S
 //     O += P V   (tcgen05, P read from tensor memory, V as it lies in HBM: keys x channels)
@@ -470,6 +471,252 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
   }
 }
 
+// ------------------------------------------------------------------ accumulated attention
+// A CTA keeps a tile of 128 keys of one KV head and goes over the query tiles of the group's heads from its own tokens on:
+//     D[key][query] = K Q^T  (tcgen05)  ->  sum over the queries of 2^(d * scale - lse)
+// A thread owns a key, so that its sum never leaves its registers; three groups of four warps take the query tiles in turn and
+// are added up at the end in a fixed order.  The queries' log-sum-exps of a tile come through shared memory, where all
+// threads of a warp read the same four at a time.
+//
+// Bound.  128 x 128 logits are 512 cycles of the tensor cores and 1024 of the special-function unit: a share of the
+// exponentials is computed on the FMA pipe (exp2_poly), until both units are busy.
+//
+// Sums.  A tile's 128 terms are added in fp32, the tiles' sums with their rounding errors kept (two-part sums).
+constexpr int A_GROUPS = 3, A_THREADS = A_GROUPS * 128 + 128, A_BUFS = 4, A_STAGES = 4;
+constexpr int A_TMA = A_GROUPS * 4, A_MMA = A_TMA + 1, A_LSE = A_TMA + 2;
+
+template <int D> constexpr size_t acc_smem() {
+  return 1024 + (size_t)(1 + A_STAGES) * (D / 64) * SLAB + A_BUFS * 128 * sizeof(float) + A_GROUPS * 128 * sizeof(float) + 256;
+}
+struct AccSmem {
+  uint8_t *k, *q;
+  float *nl, *part;                              // [A_BUFS][128] -lse * log2(e) of a tile's queries; [A_GROUPS][128] sums
+  uint64_t *k_full, *q_full, *q_empty, *acc_full, *acc_empty, *nl_full;
+  uint32_t* tmem;
+};
+template <int D>
+__device__ __forceinline__ AccSmem carve_acc(uint8_t* base) {
+  AccSmem s;
+  constexpr int TB = (D / 64) * SLAB;
+  uint8_t* p = (uint8_t*)(((uintptr_t)base + 1023) & ~(uintptr_t)1023);
+  s.k = p;                      p += TB;
+  s.q = p;                      p += A_STAGES * TB;
+  s.nl = (float*)p;             p += A_BUFS * 128 * sizeof(float);
+  s.part = (float*)p;           p += A_GROUPS * 128 * sizeof(float);
+  s.k_full = (uint64_t*)p;      p += 8;
+  s.q_full = (uint64_t*)p;      p += 8 * A_STAGES;
+  s.q_empty = (uint64_t*)p;     p += 8 * A_STAGES;
+  s.acc_full = (uint64_t*)p;    p += 8 * A_BUFS;
+  s.acc_empty = (uint64_t*)p;   p += 8 * A_BUFS;
+  s.nl_full = (uint64_t*)p;     p += 8 * A_BUFS;
+  s.tmem = (uint32_t*)p;
+  return s;
+}
+
+struct AccParams {
+  const float* lse;
+  float* out;
+  int64_t T;
+  int32_t* status;
+  long long limit;
+  int Hq, Hkv, G;
+  int q_head_step, q_token_step;
+  float scale2;
+};
+
+// This thread's key against 32 queries: the sum of its weights.  kEdge: queries before the key, or beyond the prompt, do not
+// count (whatever their logits are).
+template <bool kEdge>
+__device__ __forceinline__ void weigh32(const uint32_t (&r)[32], const float* nl, f32x2 sc, int first, int past, f32x2& acc0, f32x2& acc1) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 8) {
+    float e[8];
+    const float4 n0 = *reinterpret_cast<const float4*>(nl + c), n1 = *reinterpret_cast<const float4*>(nl + c + 4);
+    const float n[8] = {n0.x, n0.y, n0.z, n0.w, n1.x, n1.y, n1.z, n1.w};
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const f32x2 x = fma2(pack2(__uint_as_float(r[c + i]), __uint_as_float(r[c + i + 1])), sc, pack2(n[i], n[i + 1]));
+      if (i == 6 || (i == 2 && c % 16 == 0)) {   // three eighths of the exponentials on the FMA pipe
+        exp2_poly(x, e[i], e[i + 1]);
+      } else {
+        float a, b;
+        unpack2(x, a, b);
+        e[i] = ex2(a);
+        e[i + 1] = ex2(b);
+      }
+    }
+    if constexpr (kEdge) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = c + i >= first && c + i < past ? e[i] : 0.f;
+    }
+    acc0 = add2(acc0, pack2(e[0], e[1]));
+    acc1 = add2(acc1, pack2(e[2], e[3]));
+    acc0 = add2(acc0, pack2(e[4], e[5]));
+    acc1 = add2(acc1, pack2(e[6], e[7]));
+  }
+}
+template <bool kEdge>
+__device__ __forceinline__ float weigh_tile(uint32_t taddr, const float* nl, float scale2, int first, int past) {
+  const f32x2 sc = splat(scale2);
+  f32x2 acc0 = splat(0.f), acc1 = splat(0.f);
+  uint32_t a[32], b[32];
+  tmem_ld32(taddr, a);
+  tmem_wait_ld32(a);
+  tmem_ld32(taddr + 32, b);                      // the next columns are on their way during the arithmetic
+  weigh32<kEdge>(a, nl, sc, first, past, acc0, acc1);
+  tmem_wait_ld32(b);
+  tmem_ld32(taddr + 64, a);
+  weigh32<kEdge>(b, nl + 32, sc, first - 32, past - 32, acc0, acc1);
+  tmem_wait_ld32(a);
+  tmem_ld32(taddr + 96, b);
+  weigh32<kEdge>(a, nl + 64, sc, first - 64, past - 64, acc0, acc1);
+  tmem_wait_ld32(b);
+  weigh32<kEdge>(b, nl + 96, sc, first - 96, past - 96, acc0, acc1);
+  float x0, x1, x2, x3;
+  unpack2(acc0, x0, x1);
+  unpack2(acc1, x2, x3);
+  return (x0 + x1) + (x2 + x3);
+}
+
+template <int D>
+__global__ void __launch_bounds__(A_THREADS, 1)
+accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ PromptBatch B,
+              const AccParams P) {
+  constexpr int SLABS = D / 64, TB = SLABS * SLAB;
+  extern __shared__ uint8_t smem_raw[];
+  const AccSmem S = carve_acc<D>(smem_raw);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int tile = blockIdx.x / P.Hkv, g = blockIdx.x % P.Hkv;
+  const int r = request_of(B, tile), N = B.len[r], key0 = (tile - B.first[r]) * TILE;      // the first keys have the most queries
+  const int64_t cu = B.cu[r];
+  const int per_head = (N - key0 + TILE - 1) / TILE, n_tiles = per_head * P.G;      // query tiles: head by head
+
+  if (threadIdx.x == 0) {
+    mbar_init(S.k_full, 1);
+    for (int i = 0; i < A_STAGES; ++i) { mbar_init(&S.q_full[i], 1); mbar_init(&S.q_empty[i], 1); }
+    for (int i = 0; i < A_BUFS; ++i) { mbar_init(&S.acc_full[i], 1); mbar_init(&S.acc_empty[i], 4); mbar_init(&S.nl_full[i], 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == A_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(S.tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *S.tmem;
+
+  if (warp == A_TMA) {
+    mbar_expect_tx(S.k_full, TB);
+    tma_load_3d(S.k, &k_map, S.k_full, 0, (int)(g * P.T + cu) + key0, 0);
+    bool ok = true;
+    int issued = 0, h = g * P.G, q0 = key0;
+    for (int t = 0; t < n_tiles; ++t) {
+      const int s = t % A_STAGES;
+      ok = mbar_wait(&S.q_empty[s], ((uint32_t)(t / A_STAGES) & 1u) ^ 1u, P.status, P.limit);
+      if (!ok) break;
+      mbar_expect_tx(&S.q_full[s], TB);
+#pragma unroll
+      for (int sl = 0; sl < SLABS; ++sl)
+        tma_load_4d(S.q + s * TB + sl * SLAB, &q_map, &S.q_full[s], 64 * sl, (int)(cu + q0) * P.q_token_step, h * P.q_head_step, 0);
+      issued = t + 1;
+      q0 += TILE;
+      if (q0 >= N) { q0 = key0; ++h; }
+    }
+    // do not leave the CTA while a copy may still be writing its shared memory
+    mbar_wait(S.k_full, 0, P.status, P.limit);
+    for (int t = max(0, issued - A_STAGES); t < issued; ++t)
+      mbar_wait(&S.q_full[t % A_STAGES], (uint32_t)(t / A_STAGES) & 1u, P.status, P.limit);
+  } else if (warp == A_MMA) {
+    const uint32_t id = instr_desc(TILE, TILE);
+    const uint32_t a = (smem_u32(S.k) & 0x3FFFFu) >> 4, q_lo = (smem_u32(S.q) & 0x3FFFFu) >> 4;
+    bool ok = mbar_wait(S.k_full, 0, P.status, P.limit);
+    int last = -1;
+    for (int t = 0; ok && t < n_tiles; ++t) {
+      const int s = t % A_STAGES, buf = t % A_BUFS;
+      ok = mbar_wait(&S.acc_empty[buf], ((uint32_t)(t / A_BUFS) & 1u) ^ 1u, P.status, P.limit);
+      if (ok) ok = mbar_wait(&S.q_full[s], (uint32_t)(t / A_STAGES) & 1u, P.status, P.limit);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t b = q_lo + (uint32_t)(s * TB >> 4), d = tmem + 128u * buf;
+      umma_ss<0>(d, a, b, id);
+      umma_ss<1>(d, a + 2, b + 2, id);
+      umma_ss<1>(d, a + 4, b + 4, id);
+      umma_ss<1>(d, a + 6, b + 6, id);
+      if constexpr (D == 128) {
+        constexpr uint32_t o = SLAB >> 4;
+        umma_ss<1>(d, a + o, b + o, id);
+        umma_ss<1>(d, a + o + 2, b + o + 2, id);
+        umma_ss<1>(d, a + o + 4, b + o + 4, id);
+        umma_ss<1>(d, a + o + 6, b + o + 6, id);
+      }
+      umma_commit(&S.q_empty[s]);
+      umma_commit(&S.acc_full[buf]);
+      last = t;
+    }
+    // what was issued ends before tensor and shared memory are given back
+    if (last >= 0) mbar_wait(&S.acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status, P.limit);
+  } else if (warp == A_LSE) {
+    // -lse * log2(e) of the queries of every tile, three tiles ahead in registers
+    constexpr int AHEAD = 3;
+    float x[AHEAD][4];
+    auto get = [&](int t, float (&v)[4]) {
+      const int h = g * P.G + t / per_head, q0 = key0 + (t % per_head) * TILE;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = q0 + 32 * e + lane;
+        v[e] = t < n_tiles && i < N ? -P.lse[h * P.T + cu + i] * kLog2E : 0.f;
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) get(u, x[u]);
+    bool ok = true;
+    for (int t0 = 0; t0 < n_tiles && ok; t0 += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int t = t0 + u, buf = t % A_BUFS;
+        if (t >= n_tiles || !ok) break;
+        ok = mbar_wait(&S.acc_empty[buf], ((uint32_t)(t / A_BUFS) & 1u) ^ 1u, P.status, P.limit);
+        if (!ok) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S.nl[buf * 128 + 32 * e + lane] = x[u][e];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.nl_full[buf]);
+        get(t + AHEAD, x[u]);
+      }
+    }
+  } else if (warp < A_TMA) {
+    const int grp = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    float hi = 0.f, lo = 0.f;
+    for (int t = grp; t < n_tiles; t += A_GROUPS) {
+      const int buf = t % A_BUFS, q0 = key0 + (t % per_head) * TILE;
+      const uint32_t ph = (uint32_t)(t / A_BUFS) & 1u;
+      if (!mbar_wait(&S.nl_full[buf], ph, P.status, P.limit) || !mbar_wait(&S.acc_full[buf], ph, P.status, P.limit)) break;
+      tc_fence_after();
+      const uint32_t at = tmem + lanes + 128u * buf;
+      const float x = q0 == key0 || q0 + TILE > N ? weigh_tile<true>(at, S.nl + buf * 128, P.scale2, q0 == key0 ? row : 0, N - q0)
+                                                  : weigh_tile<false>(at, S.nl + buf * 128, P.scale2, 0, 0);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.acc_empty[buf]);
+      const float y = hi + x;
+      lo += hi >= x ? (hi - y) + x : (x - y) + hi;
+      hi = y;
+    }
+    S.part[grp * 128 + row] = hi + lo;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == A_MMA) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  } else if (threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
+    P.out[g * P.T + cu + key0 + threadIdx.x] =
+        ((S.part[threadIdx.x] + S.part[128 + threadIdx.x]) + S.part[256 + threadIdx.x]) * (1.f / (float)P.G);
+  }
+}
+
 // ------------------------------------------------------------------ host
 bool encode(CUtensorMap* map, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
   const EncodeTiledFn enc = encode_fn();
@@ -535,6 +782,39 @@ int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const v
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {
     fill_prompt_batch(ctx, lo, 2 * TILE, B);
     CAKE_CUDA_TRY(c.head_dim == 128 ? run_prompt_tc<128>(ctx, qm, km, vm, B, P, st) : run_prompt_tc<64>(ctx, qm, km, vm, B, P, st));
+  }
+  return CAKE_OK;
+}
+
+template <int D>
+static cudaError_t run_accumulate_tc(const cake_ctx* ctx, const CUtensorMap& qm, const CUtensorMap& km, const PromptBatch& B,
+                                     const AccParams& P, cudaStream_t st) {
+  static PerDeviceOnce once;
+  if (once.need(ctx->device)) {
+    const cudaError_t e = cudaFuncSetAttribute(accumulate_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)acc_smem<D>());
+    if (e != cudaSuccess) return e;
+    once.mark(ctx->device);
+  }
+  accumulate_tc<D><<<(unsigned)(B.tiles * P.Hkv), A_THREADS, acc_smem<D>(), st>>>(qm, km, B, P);
+  count_launch();
+  return cudaGetLastError();
+}
+
+int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
+                             cudaStream_t st) {
+  const cake_config& c = ctx->cfg;
+  CUtensorMap qm, km;
+  if (!encode_q(&qm, q, ctx, qs) || !encode_rows(&km, k, c.n_kv_heads * ctx->total_tokens, c.head_dim)) return CAKE_ERR_CUDA;
+  AccParams P;
+  P.lse = lse; P.out = out; P.T = ctx->total_tokens; P.status = ctx->d_status;
+  P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
+  P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.G = c.n_q_heads / c.n_kv_heads;
+  P.q_head_step = qs.head != 0; P.q_token_step = qs.token != 0;
+  P.scale2 = kLog2E / sqrtf((float)c.head_dim);
+  PromptBatch B;
+  for (int lo = 0; lo < ctx->n_req; lo += B.n) {
+    fill_prompt_batch(ctx, lo, TILE, B);
+    CAKE_CUDA_TRY(c.head_dim == 128 ? run_accumulate_tc<128>(ctx, qm, km, B, P, st) : run_accumulate_tc<64>(ctx, qm, km, B, P, st));
   }
   return CAKE_OK;
 }
