@@ -20,7 +20,7 @@ PY_SOURCE = os.path.join(CSRC, "py_args.cpp")
 
 SOURCES = ["cake_api.cu", "score_simt.cu", "score_tc.cu", "cascade.cu", "compact.cu",
            "decode.cu", "quant.cu", "select_static.cu", "attend_simt.cu", "attend_tc.cu",
-           "attend_cache.cu"]
+           "attend_cache.cu", "attend_rows.cu"]
 
 
 def binding_path() -> str:

@@ -39,6 +39,24 @@ struct Strided {
   int64_t head, token;
 };
 
+// Cached rows of one layer and the queries of one token per request.  group: channels (and rows) that share a scale in 4 bits,
+// 0 for rows of the context's type.
+struct CacheParams {
+  const void *q, *k, *v;             // v, k: packed rows, or their codes
+  const float *k_scale, *k_zero, *v_scale, *v_zero;
+  const int64_t *row_off, *group_off;
+  const void *k_tail, *v_tail;
+  const int32_t* tail_len;
+  int64_t tail_cap;
+  void* out;
+  float* lse;
+  int n_layers, layer, Hq, Hkv, group;
+  float scale2, scale;
+};
+
+// attend_rows.cu
+int64_t rows_workspace(const cake_ctx* ctx);
+int32_t launch_rows(const cake_ctx* ctx, int32_t n_req, const CacheParams& c, void* workspace, cudaStream_t st);
 // attend_tc.cu
 bool prompt_tc_supported(const cake_ctx* ctx, Strided q);
 int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,

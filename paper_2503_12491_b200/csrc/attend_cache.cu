@@ -15,19 +15,6 @@ namespace {
 constexpr int WARPS = 8;
 constexpr int MAXG = 8;              // query heads per KV head (cake_create allows no more)
 
-struct CacheParams {
-  const void *q, *k, *v;             // v, k: packed rows, or their codes
-  const float *k_scale, *k_zero, *v_scale, *v_zero;
-  const int64_t *row_off, *group_off;
-  const void *k_tail, *v_tail;
-  const int32_t* tail_len;
-  int64_t tail_cap;
-  void* out;
-  float* lse;
-  int n_layers, layer, Hq, Hkv, group;
-  float scale2, scale;
-};
-
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
@@ -146,7 +133,7 @@ int32_t common_args(const cake_ctx* ctx, int32_t n_req, int32_t layer, const voi
   P = {};
   P.q = q; P.row_off = row_offsets; P.out = out;
   if (tail_capacity > 0) { P.k_tail = k_tail; P.v_tail = v_tail; P.tail_len = tail_len; P.tail_cap = tail_capacity; }
-  P.n_layers = c.n_layers; P.layer = layer; P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.group = 1;
+  P.n_layers = c.n_layers; P.layer = layer; P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads;
   P.scale = 1.f / sqrtf((float)c.head_dim);
   P.scale2 = kLog2E / sqrtf((float)c.head_dim);
   return CAKE_OK;
@@ -161,7 +148,7 @@ extern "C" {
 
 int64_t cake_attend_workspace_bytes(const cake_ctx* ctx, int32_t n_req) {
   if (!ctx || n_req < 0) return CAKE_ERR_ARG;
-  return 16;
+  return std::max<int64_t>(16, rows_workspace(ctx));
 }
 
 int32_t cake_attend_cache(const cake_ctx* ctx, int32_t n_req, int32_t layer, const void* q, const void* k_cache,
@@ -174,6 +161,7 @@ int32_t cake_attend_cache(const cake_ctx* ctx, int32_t n_req, int32_t layer, con
   if (rc != CAKE_OK || n_req == 0) return rc;
   if (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)) return CAKE_ERR_ARG;
   P.k = k_cache; P.v = v_cache; P.lse = lse;
+  if (ctx->cfg.dtype == CAKE_DTYPE_BF16) return launch_rows(ctx, n_req, P, workspace, (cudaStream_t)stream);
   return launch_attend_rows<false>(ctx, n_req, P, (cudaStream_t)stream);
 }
 
@@ -194,6 +182,7 @@ int32_t cake_attend_int4(const cake_ctx* ctx, int32_t n_req, int32_t layer, cons
   P.k = k_codes; P.v = v_codes; P.lse = lse;
   P.k_scale = k_scale; P.k_zero = k_zero; P.v_scale = v_scale; P.v_zero = v_zero; P.group = group;
   P.group_off = kgroup_offsets;
+  if (ctx->cfg.dtype == CAKE_DTYPE_BF16) return launch_rows(ctx, n_req, P, workspace, (cudaStream_t)stream);
   return launch_attend_rows<true>(ctx, n_req, P, (cudaStream_t)stream);
 }
 
