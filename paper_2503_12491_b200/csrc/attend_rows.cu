@@ -1,5 +1,6 @@
 // Attention of one new token per request over its cached rows, bf16 queries: the rows in bf16 or in 4 bits.
 #include "cache_mma.cuh"
+#include "tc_ptx.cuh"
 
 namespace cake {
 namespace {
@@ -15,13 +16,15 @@ namespace {
 //
 // Products (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the query heads as the 8 columns.  With
 // up to four heads the columns 4 to 7 hold the same heads once more, for the second term of what is held in two bf16 terms
-// (kTwo): weights, and in the 4-bit kernel queries times scales, are then exact to 2^-16.  With more heads the 4-bit kernel
-// multiplies twice and the weights of the bf16 kernel are rounded to bf16.
+// (kTwo): the weights of bf16 rows, and queries times scales, are then exact to 2^-16.  With more heads the 4-bit kernel
+// multiplies the keys twice; weights are rounded to bf16, and so are, with any number of heads, weights times scales.
 //
-// 4-bit rows.  A code c becomes the bf16 16 + c by one shift and one logical operation per pair (the mantissa's upper four
-// bits); scales and zeros are never applied to a row but to the other operand: q_c s_c for the keys, p_j s_j for the values, and
-//     q.k = sum_c (q_c s_c)(16 + code) + sum_c q_c (z_c - 16 s_c) ,   p.v = sum_j (p_j s_j)(16 + code) + sum_j p_j (z_j - 16 s_j) .
-// Channels and keys are taken in whatever order the words bring them, the same one in both operands; a value tile's 16
+// 4-bit rows.  A code c becomes the bf16 16 + c (or 128 + c) by a logical operation per pair and at most one shift; scales and
+// zeros are never applied to a row but to the other operand: q_c s_c for the keys, p_j s_j for the values, and
+//     q.k = sum_c (q_c s_c)(code - 8) + sum_c q_c (z_c + 8 s_c) ,   p.v = sum_j (p_j s_j)(code - 8) + sum_j p_j (z_j + 8 s_j) .
+// What was added to the codes, and the 8, which makes the rounding of the other operand count as little as it can, comes off by
+// products of that rounded operand with a constant (the tensor cores are idle for the most part; logical operations set the
+// pace).  Channels and keys are taken in whatever order the words bring them, the same one in both operands; a value tile's 16
 // channels come from one group of 32, which has one scale per row.
 constexpr float kRefSlack = 8.f;                 // powers of two a maximum may lie above the reference before all is rescaled
 
@@ -52,7 +55,8 @@ __device__ __forceinline__ Lengths lengths_of(const CacheParams& c, int r) {
   const int64_t block = (int64_t)r * c.n_layers + c.layer;
   Lengths x;
   x.first = c.row_off[block];
-  x.n = max((int64_t)0, (c.row_off[block + 1] - x.first) / c.Hkv);
+  const int64_t rows = max((int64_t)0, c.row_off[block + 1] - x.first);
+  x.n = rows >> 32 ? rows / c.Hkv : (int64_t)((uint32_t)rows / (uint32_t)c.Hkv);
   x.kgroup = c.group_off ? c.group_off[block] : 0;
   x.tail = c.tail_cap ? (int32_t)max((int64_t)0, min((int64_t)c.tail_len[r], c.tail_cap)) : 0;
   return x;
@@ -60,17 +64,39 @@ __device__ __forceinline__ Lengths lengths_of(const CacheParams& c, int r) {
 template <int UNIT, int TAIL>
 __device__ __forceinline__ int units_of(const Lengths& x) { return (int)((x.n + UNIT - 1) / UNIT) + (x.tail + TAIL - 1) / TAIL; }
 
-// Sum of v over the block; every thread gets it.
-__device__ __forceinline__ int block_sum(int v, int* buf) {
+// Sum of v over the lanes up to this one.
+__device__ __forceinline__ int lanes_before(int v, int lane) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0;
-  for (int i = 0; i < (int)(blockDim.x >> 5); ++i) v += buf[i];
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
   return v;
 }
+// Units of 32 requests at a time, by a whole warp: the lengths of this lane's request, the sum of units up to it, all requests'.
+template <int UNIT, int TAIL>
+struct Requests {
+  Lengths len;
+  int units, upto, all;
+  __device__ __forceinline__ void read(const CacheParams& c, int n_req, int base, int lane) {
+    len = Lengths{};
+    units = 0;
+    if (base + lane < n_req) {
+      len = lengths_of(c, base + lane);
+      units = units_of<UNIT, TAIL>(len);
+    }
+    upto = lanes_before(units, lane);
+  }
+  __device__ __forceinline__ void read_all(const CacheParams& c, int n_req, int lane) {
+    all = 0;
+    for (int base = 32; base < n_req; base += 32) {
+      read(c, n_req, base, lane);
+      all += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    read(c, n_req, 0, lane);
+    all += __shfl_sync(0xffffffffu, upto, 31);
+  }
+};
 // (Units are counted in 32 bits: 2^31 of them are 4 TB of 4-bit rows.)
 __device__ __forceinline__ int per_cta(int units, int ctas) { return max(1, (units + ctas - 1) / ctas); }
 
@@ -81,10 +107,29 @@ struct Cursor {
   int r, g;
   int start, units;                              // first unit of the pair, and how many it has
   Lengths len;
-  __device__ __forceinline__ void open(const CacheParams& c, int req, int first_unit) {
-    r = req; g = 0; start = first_unit;
-    len = lengths_of(c, r);
-    units = units_of<C::UNIT, C::TAIL>(len);
+  // At the pair of unit u, by a whole warp.
+  __device__ __forceinline__ void open(const CacheParams& c, int n_req, Requests<C::UNIT, C::TAIL>& Q, int u, int lane) {
+    int before = 0;
+    for (int base = 0; ; base += 32) {
+      const uint32_t found = __ballot_sync(0xffffffffu, (before + Q.upto) * c.Hkv > u);
+      if (found) {
+        const int at = __ffs(found) - 1;
+        r = base + at; g = 0;
+        units = __shfl_sync(0xffffffffu, Q.units, at);
+        start = (before + __shfl_sync(0xffffffffu, Q.upto, at) - units) * c.Hkv;
+        len.first = __shfl_sync(0xffffffffu, Q.len.first, at);
+        len.n = __shfl_sync(0xffffffffu, Q.len.n, at);
+        len.kgroup = __shfl_sync(0xffffffffu, Q.len.kgroup, at);
+        len.tail = __shfl_sync(0xffffffffu, Q.len.tail, at);
+        const int heads = (u - start) / units;
+        g = heads;
+        start += heads * units;
+        return;
+      }
+      before += __shfl_sync(0xffffffffu, Q.upto, 31);
+      if (base + 32 >= n_req) return;                // (u is one of the units: not reached)
+      Q.read(c, n_req, base + 32, lane);
+    }
   }
   __device__ __forceinline__ void next(const CacheParams& c, int n_req) {
     start += units;
@@ -109,14 +154,15 @@ struct RowsSmem {
   static constexpr int HEADS = kTwo ? 4 : 8, PK = 36;                            // floats of a head's weights of a unit (padded)
   static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * HEADS * PK * 4, OUT = (size_t)W * HEADS * D * 4,
                           ZERO = (size_t)W * HEADS * C::NG * 4, STATS = (size_t)W * HEADS * 8;
-  static constexpr size_t BYTES = RING + WEIGHTS + OUT + ZERO + STATS + 512;
+  static constexpr size_t BYTES = RING + WEIGHTS + OUT + ZERO + STATS;
 };
 
 // A warp's running softmax: reference and (this lane's part of the) sum of the two heads of its columns 2 j, 2 j + 1, outputs
 // as the products leave them, and for 4-bit rows the sums of weights times zeros of the head of column lane / 4.
 template <int D, int NG>
 struct Running {
-  float ref[2], sum[2], o[D / 16][4], z[NG];
+  float ref[2], sum[2], o[D / 16][4];
+  f32x2 z[(NG + 1) / 2];
   __device__ __forceinline__ void clear() {
     ref[0] = ref[1] = -CUDART_INF_F;
     sum[0] = sum[1] = 0.f;
@@ -125,7 +171,7 @@ struct Running {
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NG; ++i) z[i] = 0.f;
+    for (int i = 0; i < (NG + 1) / 2; ++i) z[i] = pack2(0.f, 0.f);
   }
 };
 
@@ -138,8 +184,8 @@ __device__ __forceinline__ void weigh(Running<D, NG>& R, float (&s)[MT][4], int 
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int key = 16 * m + (lane >> 2) + 8 * (e >> 1);
-      s[m][e] = key < valid ? s[m][e] * scale2 : -CUDART_INF_F;
+      s[m][e] *= scale2;
+      if (valid < 16 * MT && 16 * m + (lane >> 2) + 8 * (e >> 1) >= valid) s[m][e] = -CUDART_INF_F;
       top[e & 1] = fmaxf(top[e & 1], s[m][e]);
     }
 #pragma unroll
@@ -164,7 +210,7 @@ __device__ __forceinline__ void weigh(Running<D, NG>& R, float (&s)[MT][4], int 
     const int col = kTwo ? (lane >> 2) & 3 : lane >> 2;
     const float a = __shfl_sync(0xffffffffu, f[0], col >> 1), b = __shfl_sync(0xffffffffu, f[1], col >> 1);
 #pragma unroll
-    for (int i = 0; i < NG; ++i) R.z[i] *= col & 1 ? b : a;
+    for (int i = 0; i < (NG + 1) / 2; ++i) R.z[i] = mul2(R.z[i], pack2(col & 1 ? b : a, col & 1 ? b : a));
   }
   const int j = lane & 3;
 #pragma unroll
@@ -234,200 +280,225 @@ __device__ __forceinline__ void dense_unit(Running<D, NG>& R, const uint32_t (&q
   __syncwarp();
 }
 
-// (16 + code) of the nibbles i and i + 4 of a word, as bf16.
+// Nibbles I and I + 4 of a word as bf16: 128 + code for the first (in the mantissa's lowest bits, no shift), else 16 + code; and
+// minus what that is for a code of 8.
 template <int I> __device__ __forceinline__ uint32_t codes(uint32_t w) {
-  const uint32_t x = I == 0 ? w << 3 : w >> (4 * I - 3 > 0 ? 4 * I - 3 : 0);
-  return (x & 0x00780078u) | 0x41804180u;
+  return I == 0 ? (w & 0x000F000Fu) | 0x43004300u : ((w >> (I ? 4 * I - 3 : 0)) & 0x00780078u) | 0x41804180u;
 }
+template <int I> constexpr uint32_t kMinusMid = I == 0 ? 0xC308C308u : 0xC1C0C1C0u;      // -136, -24
 
-// 32 rows in 4 bits.  qf: queries of the head of column lane / 4, channels of quarter lane % 4 of a row.
+// 32 rows in 4 bits.  qf: queries of the head of column lane / 4, pairs of channels of quarter lane % 4 of a row (with kTwo the
+// half of them that this lane works on).  With kTwo the
+// lanes of columns i and i + 4, which have the same head, share the work on the other operands: each takes half of the channels (of
+// the keys) and hands the other the part of its results that this one multiplies with.
 template <int D, int GROUP, bool kTwo, int PK>
-__device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const float (&qf)[D / 4], const uint8_t* st, int valid, float scale2, float* sp,
+__device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 (&qf)[D / (kTwo ? 16 : 8)], uint32_t st, int valid, float scale2, float* sp,
                                           int lane) {
   using C = RowsCfg<D, GROUP>;
   constexpr int NG = C::NG, WORDS = D / 32;        // words of a quarter of a row
   const int n = lane >> 2, j = lane & 3;
   const bool second = n >= 4;
-  const uint8_t *kc = st, *vc = st + C::K_BYTES;
-  const float *ks = (const float*)(st + 2 * C::K_BYTES), *kz = ks + D, *vs = kz + D, *vz = vs + C::UNIT * NG;
-  // --- keys: the queries times the scales of the unit's group, and the part that the zeros give
-  uint32_t b[D / 16][2], b2[kTwo ? 1 : D / 16][2];
-  float2 bias = make_float2(0.f, 0.f);
+  const uint32_t kc = st, vc = st + C::K_BYTES, ks = st + 2 * C::K_BYTES, kz = ks + D * 4, vs = kz + D * 4, vz = vs + C::UNIT * NG * 4;
+  // --- keys: the queries times the scales of the unit's group in two bf16 terms, and what the zeros and middles give
+  uint32_t b[D / 16][2], b2[D / 16][2];              // (kTwo: b alone is multiplied with)
+  f32x2 bias = pack2(0.f, 0.f);
+  constexpr int MINE = kTwo ? WORDS / 2 : WORDS;
 #pragma unroll
-  for (int w = 0; w < WORDS; ++w) {
-    float x[8];
+  for (int u = 0; u < MINE; ++u) {
+    const int w = kTwo && second ? u + WORDS / 2 : u;
+    float x[8], r[8];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int c = j * (D / 16) + 2 * w + u, at = ((c & ~7) | ((c ^ (c >> 3)) & 7)) * 4;      // 16-byte piece, see load_int4
-      const float4 sc = *reinterpret_cast<const float4*>(ks + at), ze = *reinterpret_cast<const float4*>(kz + at);
-      const float* q = qf + 8 * w + 4 * u;
-      x[4 * u] = q[0] * sc.x; x[4 * u + 1] = q[1] * sc.y; x[4 * u + 2] = q[2] * sc.z; x[4 * u + 3] = q[3] * sc.w;
-      bias.x = fmaf(q[0], fmaf(-16.f, sc.x, ze.x), bias.x);
-      bias.y = fmaf(q[1], fmaf(-16.f, sc.y, ze.y), bias.y);
-      bias.x = fmaf(q[2], fmaf(-16.f, sc.z, ze.z), bias.x);
-      bias.y = fmaf(q[3], fmaf(-16.f, sc.w, ze.w), bias.y);
+    for (int e = 0; e < 2; ++e) {
+      const int c = j * (D / 16) + 2 * w + e, at = ((c & ~7) | ((c ^ (c >> 3)) & 7)) * 16;     // 16-byte piece, see load_int4
+      f32x2 sc[2], ze[2];
+      ld_shared2(sc, ks + at);
+      ld_shared2(ze, kz + at);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x2 q = qf[4 * u + 2 * e + i];
+        const f32x2 y = mul2(q, sc[i]);
+        bias = fma2(q, fma2(pack2(8.f, 8.f), sc[i], ze[i]), bias);
+        float y0, y1;
+        unpack2(y, y0, y1);
+        const int at8 = 4 * e + 2 * i;
+        x[at8] = bf16_floor(y0); x[at8 + 1] = bf16_floor(y1);
+        unpack2(fma2(pack2(x[at8], x[at8 + 1]), pack2(-1.f, -1.f), y), r[at8], r[at8 + 1]);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {                  // channels i and i + 4 of the word
-      const float lo = bf16_floor(x[i]), hi = bf16_floor(x[i + 4]);
+      const uint32_t lead = bf16_pair(x[i], x[i + 4]), rest = bf16_pair(r[i], r[i + 4]);
       if constexpr (kTwo) {
-        b[2 * w + i / 2][i & 1] = bf16_pair(second ? x[i] - lo : lo, second ? x[i + 4] - hi : hi);
+        const uint32_t keep = second ? rest : lead, got = __shfl_xor_sync(0xffffffffu, second ? lead : rest, 16);
+        // the first lane worked on word u and gets word u + WORDS / 2, the second the other way round
+        b[2 * u + i / 2][i & 1] = second ? got : keep;
+        b[2 * (u + WORDS / 2) + i / 2][i & 1] = second ? keep : got;
       } else {
-        b[2 * w + i / 2][i & 1] = bf16_pair(lo, hi);
-        b2[2 * w + i / 2][i & 1] = bf16_pair(x[i] - lo, x[i + 4] - hi);
+        b[2 * u + i / 2][i & 1] = lead;
+        b2[2 * u + i / 2][i & 1] = rest;
       }
     }
   }
-  float bi = bias.x + bias.y;
+  float bi, bi1;
+  unpack2(bias, bi, bi1);
+  bi += bi1;
   bi += __shfl_xor_sync(0xffffffffu, bi, 1);
   bi += __shfl_xor_sync(0xffffffffu, bi, 2);
+  if constexpr (kTwo) bi += __shfl_xor_sync(0xffffffffu, bi, 16);
   const int c0 = kTwo ? (2 * j) & 3 : 2 * j;
-  const float bias0 = __shfl_sync(0xffffffffu, bi, 4 * c0), bias1 = __shfl_sync(0xffffffffu, bi, 4 * c0 + 4);
-  float s[2][4];
+  float bias0 = __shfl_sync(0xffffffffu, bi, 4 * c0), bias1 = __shfl_sync(0xffffffffu, bi, 4 * c0 + 4);
+  // with kTwo both terms are added up below, and these must come in once
+  if (kTwo && j >= 2) bias0 = bias1 = 0.f;
+  // chains of products that do not wait for one another: two per tile of keys, two for the middles
+  float s[2][4], sx[2][4] = {}, mid[4] = {bias0, bias1, bias0, bias1}, midx[4] = {};
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     s[m][0] = s[m][1] = s[m][2] = s[m][3] = 0.f;
     uint32_t a[WORDS], c[WORDS];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int row = 16 * m + n + 8 * half;
-      uint32_t* to = half ? c : a;
-      if constexpr (D == 128) {
-        const uint4 v = *reinterpret_cast<const uint4*>(kc + row * 64 + ((j ^ ((row >> 1) & 3)) << 4));
-        to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(kc + row * 32 + j * 8);
-        to[0] = v.x; to[1] = v.y;
-      }
+    const int row = 16 * m + n;
+    if constexpr (D == 128) {
+      ld_shared4(a, kc + row * 64 + ((j ^ ((row >> 1) & 3)) << 4));
+      ld_shared4(c, kc + (row + 8) * 64 + ((j ^ ((row >> 1) & 3)) << 4));
+    } else {
+      ld_shared2u(a, kc + row * 32 + j * 8);
+      ld_shared2u(c, kc + (row + 8) * 32 + j * 8);
     }
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
+      constexpr uint32_t m0 = kMinusMid<0>, m1 = kMinusMid<1>;
       const uint32_t a0 = codes<0>(a[w]), a1 = codes<0>(c[w]), a2 = codes<1>(a[w]), a3 = codes<1>(c[w]);
       const uint32_t d0 = codes<2>(a[w]), d1 = codes<2>(c[w]), d2 = codes<3>(a[w]), d3 = codes<3>(c[w]);
       mma16816(s[m], a0, a1, a2, a3, b[2 * w][0], b[2 * w][1]);
-      mma16816(s[m], d0, d1, d2, d3, b[2 * w + 1][0], b[2 * w + 1][1]);
+      mma16816(sx[m], d0, d1, d2, d3, b[2 * w + 1][0], b[2 * w + 1][1]);
+      if (m == 0) {
+        mma16816(mid, m0, m0, m1, m1, b[2 * w][0], b[2 * w][1]);
+        mma16816(midx, m1, m1, m1, m1, b[2 * w + 1][0], b[2 * w + 1][1]);
+      }
       if constexpr (!kTwo) {
         mma16816(s[m], a0, a1, a2, a3, b2[2 * w][0], b2[2 * w][1]);
-        mma16816(s[m], d0, d1, d2, d3, b2[2 * w + 1][0], b2[2 * w + 1][1]);
+        mma16816(sx[m], d0, d1, d2, d3, b2[2 * w + 1][0], b2[2 * w + 1][1]);
+        if (m == 0) {
+          mma16816(mid, m0, m0, m1, m1, b2[2 * w][0], b2[2 * w][1]);
+          mma16816(midx, m1, m1, m1, m1, b2[2 * w + 1][0], b2[2 * w + 1][1]);
+        }
       }
     }
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (kTwo) s[m][e] += __shfl_xor_sync(0xffffffffu, s[m][e], 2);             // both terms
-      s[m][e] += e & 1 ? bias1 : bias0;
+      s[m][e] = (s[m][e] + sx[m][e]) + (mid[e] + midx[e]);
+      if (kTwo) s[m][e] += __shfl_xor_sync(0xffffffffu, s[m][e], 2);
     }
-  }
   weigh<D, NG, kTwo, 2, PK>(R, s, valid, scale2, sp, lane);
-  // --- values: keys j, j + 4, j + 8, j + 12 of 16
+  // --- values: keys j, j + 4, j + 8, j + 12 of 16; the weights times the scales
   const float* p = sp + (kTwo ? n & 3 : n) * PK;
+  uint32_t bb[2][NG][2];
 #pragma unroll
-  for (int kstep = 0; kstep < 2; ++kstep) {
+  for (int half = 0; half < (kTwo ? 1 : 2); ++half) {
+    const int kstep = kTwo ? second : half;
     float x[NG][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 16 * kstep + j + 4 * i;
       const float w = p[row];
-      float sc[NG], ze[NG];
-      if constexpr (NG == 4) {
-        const float4 u = *reinterpret_cast<const float4*>(vs + row * 4), v = *reinterpret_cast<const float4*>(vz + row * 4);
-        sc[0] = u.x; sc[1] = u.y; sc[2] = u.z; sc[3] = u.w;
-        ze[0] = v.x; ze[1] = v.y; ze[2] = v.z; ze[3] = v.w;
-      } else if constexpr (NG == 2) {
-        const float2 u = *reinterpret_cast<const float2*>(vs + row * 2), v = *reinterpret_cast<const float2*>(vz + row * 2);
-        sc[0] = u.x; sc[1] = u.y;
-        ze[0] = v.x; ze[1] = v.y;
-      } else {
-        sc[0] = vs[row];
-        ze[0] = vz[row];
-      }
+      if constexpr (NG > 1) {
+        f32x2 sc[NG / 2], ze[NG / 2];
+        ld_shared_n(sc, vs + row * NG * 4);
+        ld_shared_n(ze, vz + row * NG * 4);
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        x[g][i] = w * sc[g];
-        R.z[g] = fmaf(w, fmaf(-16.f, sc[g], ze[g]), R.z[g]);
+        for (int g = 0; g < NG / 2; ++g) {
+          unpack2(mul2(pack2(w, w), sc[g]), x[2 * g][i], x[2 * g + 1][i]);
+          R.z[g] = fma2(pack2(w, w), fma2(pack2(8.f, 8.f), sc[g], ze[g]), R.z[g]);
+        }
+      } else {
+        float sc, ze;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc) : "r"(vs + row * 4) : "memory");
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ze) : "r"(vz + row * 4) : "memory");
+        x[0][i] = w * sc;
+        R.z[0] = fma2(pack2(w, 0.f), pack2(fmaf(8.f, sc, ze), 0.f), R.z[0]);
       }
     }
-    uint32_t bb[NG][2], bl[kTwo ? 1 : NG][2];
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float lo = bf16_floor(x[g][2 * u]), hi = bf16_floor(x[g][2 * u + 1]);
+        const uint32_t v = bf16_pair(x[g][2 * u], x[g][2 * u + 1]);
         if constexpr (kTwo) {
-          bb[g][u] = bf16_pair(second ? x[g][2 * u] - lo : lo, second ? x[g][2 * u + 1] - hi : hi);
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, v, 16);             // the columns from 4 on stay empty
+          bb[0][g][u] = second ? 0u : v;
+          bb[1][g][u] = second ? 0u : got;
         } else {
-          bb[g][u] = bf16_pair(lo, hi);
-          bl[g][u] = bf16_pair(x[g][2 * u] - lo, x[g][2 * u + 1] - hi);
+          bb[half][g][u] = v;
         }
       }
+  }
+#pragma unroll
+  for (int kstep = 0; kstep < 2; ++kstep)
 #pragma unroll
     for (int blk = 0; blk < D / 32; ++blk) {         // 32 channels: two bytes of this lane's per row
       uint32_t h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = 16 * kstep + j + 4 * i, piece = D == 128 ? blk ^ ((row >> 1) & 3) : blk;
-        h[i] = *reinterpret_cast<const uint16_t*>(vc + row * (D / 2) + piece * 16 + 2 * n);
+        asm volatile("{\n.reg .u16 t;\nld.shared.u16 t, [%1];\ncvt.u32.u16 %0, t;\n}" : "=r"(h[i]) : "r"(vc + row * (D / 2) + piece * 16 + 2 * n) : "memory");
       }
       const uint32_t w0 = __byte_perm(h[0], h[1], 0x5410), w1 = __byte_perm(h[2], h[3], 0x5410);
-      constexpr int per = NG > 0 ? (D / 32) / NG : 1;
+      constexpr int per = (D / 32) / NG;
       const int g = blk / per;
-      const uint32_t x0 = codes<0>(w0), x1 = codes<1>(w0), x2 = codes<0>(w1), x3 = codes<1>(w1);
-      const uint32_t y0 = codes<2>(w0), y1 = codes<3>(w0), y2 = codes<2>(w1), y3 = codes<3>(w1);
-      mma16816(R.o[2 * blk], x0, x1, x2, x3, bb[g][0], bb[g][1]);
-      mma16816(R.o[2 * blk + 1], y0, y1, y2, y3, bb[g][0], bb[g][1]);
-      if constexpr (!kTwo) {
-        mma16816(R.o[2 * blk], x0, x1, x2, x3, bl[g][0], bl[g][1]);
-        mma16816(R.o[2 * blk + 1], y0, y1, y2, y3, bl[g][0], bl[g][1]);
-      }
+      mma16816(R.o[2 * blk], codes<0>(w0), codes<1>(w0), codes<0>(w1), codes<1>(w1), bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(R.o[2 * blk + 1], codes<2>(w0), codes<3>(w0), codes<2>(w1), codes<3>(w1), bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(R.o[2 * blk], kMinusMid<0>, kMinusMid<1>, kMinusMid<0>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(R.o[2 * blk + 1], kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
     }
-  }
   __syncwarp();
 }
 
 // Copies of `rows` bf16 rows (those from `valid` on read as zeros) into shared memory, 16-byte piece c of a row at c ^ (row % 8).
-template <int D>
-__device__ __forceinline__ void load_dense(uint32_t dst, const __nv_bfloat16* src, int rows, int valid, int lane) {
-  constexpr int CH = D / 8;
-#pragma unroll 8
-  for (int i = lane; i < rows * CH; i += 32) {
-    const int r = i / CH, c = i % CH;
-    copy_async16(dst + (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4)), src + (r < valid ? (int64_t)r * D + c * 8 : 0), r < valid);
+template <int D, int ROWS>
+__device__ __forceinline__ void load_dense(uint32_t dst, const __nv_bfloat16* src, int valid, int lane) {
+  constexpr int CH = D / 8, STEP = 32 / CH;
+  const int r0 = lane / CH, c = lane % CH;
+#pragma unroll
+  for (int i = 0; i < ROWS / STEP; ++i) {
+    const int r = r0 + i * STEP;
+    copy_async16n(dst + (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4)), src + lane * 8 + i * 256, r < valid ? 16 : 0);
   }
 }
 // Copies of a unit of 4-bit rows: codes (128 channels: piece c of a row at c ^ (row / 2 % 4), so that neither the keys' 16-byte
 // nor the values' 2-byte reads meet bank conflicts), the keys' scales and zeros of their group (piece c at c ^ (c / 8) within eight
 // pieces, for the same reason), the values' scales and zeros.
 template <int D, int GROUP>
-__device__ __forceinline__ void load_int4(uint8_t* st, const CacheParams& c, int64_t row, int64_t kgroup, int valid, int lane) {
+__device__ __forceinline__ void load_int4(uint32_t at, const CacheParams& c, int64_t row, int64_t kgroup, int valid, int lane) {
   using C = RowsCfg<D, GROUP>;
-  constexpr int NG = C::NG, CH = D / 32;
-  const uint32_t at = smem_addr(st);
-  const uint8_t *k = (const uint8_t*)c.k + row * (D / 2), *v = (const uint8_t*)c.v + row * (D / 2);
+  constexpr int NG = C::NG, CH = D / 32, ROWS = 32 / CH;                         // pieces of a row; rows of a pass of the warp
+  const uint8_t *k = (const uint8_t*)c.k + row * (D / 2) + lane * 16, *v = (const uint8_t*)c.v + row * (D / 2) + lane * 16;
+  const int r0 = lane / CH, p = lane % CH;
 #pragma unroll
-  for (int i = lane; i < C::UNIT * CH; i += 32) {
-    const int r = i / CH, p = i % CH;
+  for (int i = 0; i < C::UNIT / ROWS; ++i) {
+    const int r = r0 + i * ROWS;
     const uint32_t to = at + (uint32_t)(r * (D / 2) + ((D == 128 ? p ^ ((r >> 1) & 3) : p) << 4));
-    const bool in = r < valid;
-    copy_async16(to, k + (in ? i * 16 : 0), in);
-    copy_async16(to + C::K_BYTES, v + (in ? i * 16 : 0), in);
+    const int n = r < valid ? 16 : 0;                                            // beyond: zeros, nothing is read
+    copy_async16n(to, k + i * 512, n);
+    copy_async16n(to + C::K_BYTES, v + i * 512, n);
   }
   const uint32_t ks = at + 2 * C::K_BYTES, vs = ks + 2 * C::KS_BYTES;
   if (lane < D / 4) {
-    const int p = (lane & ~7) | ((lane ^ (lane >> 3)) & 7);
-    copy_async16(ks + p * 16, c.k_scale + kgroup * D + lane * 4, true);
-    copy_async16(ks + C::KS_BYTES + p * 16, c.k_zero + kgroup * D + lane * 4, true);
+    const int to = ((lane & ~7) | ((lane ^ (lane >> 3)) & 7)) * 16;
+    copy_async16n(ks + to, c.k_scale + kgroup * D + lane * 4, 16);
+    copy_async16n(ks + C::KS_BYTES + to, c.k_zero + kgroup * D + lane * 4, 16);
   }
   if constexpr (NG == 4) {                           // a row's scales start on a 16-byte boundary
-    const bool in = lane < valid;
-    const int64_t o = in ? (row + lane) * 4 : 0;
-    copy_async16(vs + lane * 16, c.v_scale + o, in);
-    copy_async16(vs + C::VS_BYTES + lane * 16, c.v_zero + o, in);
+    const int n = lane < valid ? 16 : 0;
+    copy_async16n(vs + lane * 16, c.v_scale + (row + lane) * 4, n);
+    copy_async16n(vs + C::VS_BYTES + lane * 16, c.v_zero + (row + lane) * 4, n);
   } else {
 #pragma unroll
-    for (int i = lane; i < C::UNIT * NG; i += 32) {
-      const bool in = i / NG < valid;
-      const int64_t o = in ? row * NG + i : 0;
-      copy_async4z(vs + i * 4, c.v_scale + o, in);
-      copy_async4z(vs + C::VS_BYTES + i * 4, c.v_zero + o, in);
+    for (int i = 0; i < NG; ++i) {
+      const int n = (lane + 32 * i) / NG < valid ? 4 : 0;
+      copy_async4n(vs + (lane + 32 * i) * 4, c.v_scale + row * NG + lane + 32 * i, n);
+      copy_async4n(vs + C::VS_BYTES + (lane + 32 * i) * 4, c.v_zero + row * NG + lane + 32 * i, n);
     }
   }
 }
@@ -443,40 +514,19 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   float* m_out = (float*)(smem_raw + M::RING + M::WEIGHTS);
   float* m_zero = (float*)(smem_raw + M::RING + M::WEIGHTS + M::OUT);
   float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS + M::OUT + M::ZERO);
-  int* scratch = (int*)(smem_raw + M::BYTES - 512);
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
   // merge_shares may take its places now; it waits for the end of this kernel before it reads anything of it
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // --- this CTA's units, and the pair of the first
-  int mine = 0;
-  for (int r = threadIdx.x; r < P.n_req; r += W * 32) mine += units_of<C::UNIT, C::TAIL>(lengths_of(c, r));
-  const int total = block_sum(mine, scratch) * c.Hkv, per = per_cta(total, gridDim.x);
+  Requests<C::UNIT, C::TAIL> Q;
+  Q.read_all(c, P.n_req, lane);
+  const int total = Q.all * c.Hkv, per = per_cta(total, gridDim.x);
   const int u0 = (int)min((int64_t)total, (int64_t)blockIdx.x * per), u1 = min(u0 + per, total);
   if (u0 >= u1) return;
-  if (warp == 0) {
-    int before = 0;
-    for (int base = 0; base < P.n_req; base += 32) {
-      const int v = base + lane < P.n_req ? units_of<C::UNIT, C::TAIL>(lengths_of(c, base + lane)) : 0;
-      int inc = v;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += x;
-      }
-      const uint32_t found = __ballot_sync(0xffffffffu, (before + inc) * c.Hkv > u0);
-      if (found) {
-        if (lane == __ffs(found) - 1) { scratch[32] = base + lane; scratch[33] = (before + inc - v) * c.Hkv; }
-        break;
-      }
-      before += __shfl_sync(0xffffffffu, inc, 31);
-    }
-  }
-  __syncthreads();
   Cursor<D, GROUP> load, work;
-  load.open(c, scratch[32], scratch[33]);
-  load.seek(c, P.n_req, u0);
+  load.open(c, P.n_req, Q, u0, lane);
   work = load;
 
   uint8_t* my_ring = ring + (size_t)warp * ST * C::STAGE;
@@ -490,17 +540,17 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         const int valid = (int)min((int64_t)C::UNIT, load.len.n - (int64_t)at * C::UNIT);
         const int64_t row = load.len.first + load.g * load.len.n + (int64_t)at * C::UNIT;
         if constexpr (C::INT4) {
-          load_int4<D, GROUP>(st, c, row, load.len.kgroup + load.g * ((load.len.n + GROUP - 1) / GROUP) + (int64_t)at * C::UNIT / GROUP,
+          load_int4<D, GROUP>(smem_addr(st), c, row, load.len.kgroup + load.g * ((load.len.n + GROUP - 1) / GROUP) + (int64_t)at * C::UNIT / GROUP,
                               valid, lane);
         } else {
-          load_dense<D>(smem_addr(st), (const __nv_bfloat16*)c.k + row * D, C::UNIT, valid, lane);
-          load_dense<D>(smem_addr(st) + C::K_BYTES, (const __nv_bfloat16*)c.v + row * D, C::UNIT, valid, lane);
+          load_dense<D, C::UNIT>(smem_addr(st), (const __nv_bfloat16*)c.k + row * D, valid, lane);
+          load_dense<D, C::UNIT>(smem_addr(st) + C::K_BYTES, (const __nv_bfloat16*)c.v + row * D, valid, lane);
         }
       } else {
         const int t0 = (at - packed) * C::TAIL, valid = min(C::TAIL, load.len.tail - t0);
         const int64_t row = ((int64_t)load.r * c.Hkv + load.g) * c.tail_cap + t0;
-        load_dense<D>(smem_addr(st), (const __nv_bfloat16*)c.k_tail + row * D, C::TAIL, valid, lane);
-        load_dense<D>(smem_addr(st) + C::TAIL * D * 2, (const __nv_bfloat16*)c.v_tail + row * D, C::TAIL, valid, lane);
+        load_dense<D, C::TAIL>(smem_addr(st), (const __nv_bfloat16*)c.k_tail + row * D, valid, lane);
+        load_dense<D, C::TAIL>(smem_addr(st) + C::TAIL * D * 2, (const __nv_bfloat16*)c.v_tail + row * D, valid, lane);
       }
     }
     copy_commit();
@@ -520,18 +570,23 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     const __nv_bfloat16* q = (const __nv_bfloat16*)c.q + ((int64_t)work.r * c.Hq + work.g * G + head) * D;
     const bool live = head < G;
     uint32_t qd[D / 16][2];
-    float qf[C::INT4 ? D / 4 : 1];
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      qd[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
-      qd[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
-    }
+    constexpr int QW = D / (kTwo ? 64 : 32);         // pieces of eight channels
+    f32x2 qf[C::INT4 ? 4 * QW : 1];
     if constexpr (C::INT4) {
 #pragma unroll
-      for (int i = 0; i < D / 4; i += 2) {
-        const uint32_t w = live ? *reinterpret_cast<const uint32_t*>(q + j * (D / 4) + i) : 0u;
-        qf[i] = __uint_as_float(w << 16);
-        qf[i + 1] = __uint_as_float(w & 0xFFFF0000u);
+      for (int i = 0; i < QW; ++i) {
+        const uint4 w = live ? *reinterpret_cast<const uint4*>(q + j * (D / 4) + 8 * (i + (kTwo && n >= 4 ? QW : 0))) : make_uint4(0, 0, 0, 0);
+        qf[4 * i] = pack2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u));
+        qf[4 * i + 1] = pack2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+        qf[4 * i + 2] = pack2(__uint_as_float(w.z << 16), __uint_as_float(w.z & 0xFFFF0000u));
+        qf[4 * i + 3] = pack2(__uint_as_float(w.w << 16), __uint_as_float(w.w & 0xFFFF0000u));
+      }
+    }
+    if (!C::INT4 || work.len.tail > 0) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        qd[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
+        qd[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
       }
     }
     for (; u0 + warp + k * W < end; ++k) {
@@ -542,7 +597,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
       uint8_t* st = my_ring + (size_t)(k % ST) * C::STAGE;
       if (at < packed) {
         const int valid = (int)min((int64_t)C::UNIT, work.len.n - (int64_t)at * C::UNIT);
-        if constexpr (C::INT4) int4_unit<D, GROUP, kTwo, PK>(R, qf, st, valid, c.scale2, sp, lane);
+        if constexpr (C::INT4) int4_unit<D, GROUP, kTwo, PK>(R, qf, smem_addr(st), valid, c.scale2, sp, lane);
         else dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::K_BYTES, valid, c.scale2, sp, lane);
       } else {
         const int valid = min(C::TAIL, work.len.tail - (at - packed) * C::TAIL);
@@ -573,9 +628,12 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     if constexpr (C::INT4) {
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        float x = R.z[i];
+        float x, y;
+        unpack2(R.z[i / 2], x, y);
+        if (i & 1) x = y;
         x += __shfl_xor_sync(0xffffffffu, x, 1);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
+        if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 16);
         if (j == 0 && (!kTwo || n < 4)) m_zero[(warp * HEADS + head) * NG + i] = x;
       }
     }
@@ -616,53 +674,89 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   copy_wait<0>();
 }
 
-// Pairs that lie in several CTAs, from the shares these left; and pairs without any row.
+// Pairs that lie in several CTAs, from the shares these left; and pairs without any row.  A thread sums four channels of
+// every M_PARTS-th share; what it reads first is on its way while the shares' references are compared.
+constexpr int M_THREADS = 512, M_AHEAD = 6;
 template <int D, int GROUP>
-__global__ void __launch_bounds__(128) merge_shares(const RowsParams P, int ctas) {
+__global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, int ctas) {
   using C = RowsCfg<D, GROUP>;
-  __shared__ int scratch[4];
+  extern __shared__ float m_smem[];                  // [ctas][G] factors; [M_THREADS] partial sums of four channels
+  __shared__ float s_top[8], s_sum[8];
   const CacheParams& c = P.c;
-  const int g = blockIdx.x, r = blockIdx.y, G = c.Hq / c.Hkv;
-  int all = 0, before = 0;
-  for (int x = threadIdx.x; x < P.n_req; x += 128) {
-    const int v = units_of<C::UNIT, C::TAIL>(lengths_of(c, x));
-    all += v;
-    before += x < r ? v : 0;
+  const int g = blockIdx.x, r = blockIdx.y, G = c.Hq / c.Hkv, lane = threadIdx.x & 31;
+  Requests<C::UNIT, C::TAIL> Q;
+  Q.read_all(c, P.n_req, lane);
+  const int total = Q.all * c.Hkv, per = per_cta(total, ctas);
+  int before = 0;
+  for (int base = 0; base < (r & ~31); base += 32) {
+    if (base) Q.read(c, P.n_req, base, lane);
+    before += __shfl_sync(0xffffffffu, Q.upto, 31);
   }
-  all = block_sum(all, scratch) * c.Hkv;
-  before = block_sum(before, scratch) * c.Hkv;
-  const int mine = units_of<C::UNIT, C::TAIL>(lengths_of(c, r)), start = before + g * mine, per = per_cta(all, ctas);
+  if (r >= 32) Q.read(c, P.n_req, r & ~31, lane);
+  const int mine = __shfl_sync(0xffffffffu, Q.units, r & 31);
+  const int start = (before + __shfl_sync(0xffffffffu, Q.upto, r & 31) - mine) * c.Hkv + g * mine;
   // Every CTA waits, also one with nothing to do: the end of this kernel stands for the end of the one before.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t at = (int64_t)r * c.Hq + g * G;
   if (mine == 0) {
-    for (int i = threadIdx.x; i < G * D; i += 128) ((__nv_bfloat16*)c.out)[at * D + i] = __float2bfloat16_rn(0.f);
+    for (int i = threadIdx.x; i < G * D; i += M_THREADS) ((__nv_bfloat16*)c.out)[at * D + i] = __float2bfloat16_rn(0.f);
     if (c.lse && (int)threadIdx.x < G) c.lse[at + threadIdx.x] = -CUDART_INF_F;
     return;
   }
-  const int c0 = start / per, c1 = (start + mine - 1) / per;
-  if (c0 == c1) return;
-  const float* stats = P.shares + share_stats(ctas, G, D);
-  for (int i = threadIdx.x; i < G * D / 4; i += 128) {
-    const int h = i / (D / 4), ch = i % (D / 4) * 4;
-    // (the first CTA's share is the one at the end of its run)
-    auto share = [&](int x) { return (int64_t)(2 * x + (x == c0 ? 1 : 0)) * G + h; };
-    float top = -CUDART_INF_F, sum = 0.f;
-    for (int x = c0; x <= c1; ++x) top = fmaxf(top, __ldcg(stats + share(x) * 2));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int x = c0; x <= c1; ++x) {
-      const float2 t = __ldcg(reinterpret_cast<const float2*>(stats + share(x) * 2));
-      const float4 o = __ldcg(reinterpret_cast<const float4*>(P.shares + share(x) * D + ch));
-      const float f = exp2f(t.x - top);
-      sum = fmaf(t.y, f, sum);
-      acc.x = fmaf(o.x, f, acc.x); acc.y = fmaf(o.y, f, acc.y); acc.z = fmaf(o.z, f, acc.z); acc.w = fmaf(o.w, f, acc.w);
-    }
-    const float inv = 1.f / sum;
-    uint2 w = make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
-    *reinterpret_cast<uint2*>((__nv_bfloat16*)c.out + (at + h) * D + ch) = w;
-    if (c.lse && ch == 0) c.lse[at + h] = (top + log2f(sum)) * kLn2;
+  const int c0 = start / per, n = (start + mine - 1) / per - c0 + 1;
+  if (n == 1) return;
+  // (the first CTA's share is the one at the end of its run)
+  auto share = [&](int x) { return (int64_t)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * G; };
+  const int quads = G * D / 4, parts = M_THREADS / quads, part = threadIdx.x / quads, quad = threadIdx.x % quads;
+  const int h = quad / (D / 4);
+  const float4* o = reinterpret_cast<const float4*>(P.shares) + quad;
+  float4 v[M_AHEAD];
+#pragma unroll
+  for (int u = 0; u < M_AHEAD; ++u) {
+    const int x = part + u * parts;
+    v[u] = part < parts && x < n ? __ldcg(o + share(x) * (D / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
+  const float* stats = P.shares + share_stats(ctas, G, D);
+  for (int w = threadIdx.x >> 5; w < G; w += M_THREADS / 32) {                   // a warp per head
+    float top = -CUDART_INF_F, sum = 0.f;
+    for (int x = lane; x < n; x += 32) {
+      const float2 t = __ldcg(reinterpret_cast<const float2*>(stats + (share(x) + w) * 2));
+      m_smem[x * G + w] = t.x;
+      const float to = fmaxf(top, t.x);
+      sum = fmaf(sum, top == to ? 1.f : exp2f(top - to), t.y * exp2f(t.x - to));
+      top = to;
+    }
+    float all = top;
+#pragma unroll
+    for (int y = 16; y > 0; y >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, y));
+    sum *= top == -CUDART_INF_F ? 1.f : exp2f(top - all);
+#pragma unroll
+    for (int y = 16; y > 0; y >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
+    for (int x = lane; x < n; x += 32) m_smem[x * G + w] = exp2f(m_smem[x * G + w] - all);
+    if (lane == 0) { s_top[w] = all; s_sum[w] = sum; }
+  }
+  __syncthreads();
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& y, float f) {
+    acc.x = fmaf(y.x, f, acc.x); acc.y = fmaf(y.y, f, acc.y); acc.z = fmaf(y.z, f, acc.z); acc.w = fmaf(y.w, f, acc.w);
+  };
+  if (part < parts) {
+#pragma unroll
+    for (int u = 0; u < M_AHEAD; ++u) {
+      const int x = part + u * parts;
+      if (x < n) add(v[u], m_smem[x * G + h]);
+    }
+#pragma unroll 4
+    for (int x = part + M_AHEAD * parts; x < n; x += parts) add(__ldcg(o + share(x) * (D / 4)), m_smem[x * G + h]);
+  }
+  float4* sums = reinterpret_cast<float4*>(m_smem + (ctas * G + 3) / 4 * 4);
+  sums[threadIdx.x] = acc;
+  __syncthreads();
+  if ((int)threadIdx.x >= quads) return;
+  for (int y = 1; y < parts; ++y) add(sums[y * quads + quad], 1.f);
+  const float inv = 1.f / s_sum[h];
+  reinterpret_cast<uint2*>((__nv_bfloat16*)c.out + at * D)[quad] = make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
+  if (c.lse && quad % (D / 4) == 0) c.lse[at + h] = (s_top[h] + log2f(s_sum[h])) * kLn2;
 }
 
 template <int D, int GROUP, bool kTwo, int W, int ST>
@@ -681,7 +775,8 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.c.Hkv, (unsigned)P.n_req, 1);
-  cfg.blockDim = dim3(128, 1, 1);
+  cfg.blockDim = dim3(M_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = ((size_t)ctx->n_sm * (P.c.Hq / P.c.Hkv) + 3) / 4 * 16 + M_THREADS * 16;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
