@@ -153,7 +153,7 @@ struct RowsSmem {
   using C = RowsCfg<D, GROUP>;
   static constexpr int HEADS = kTwo ? 4 : 8, PK = 36;                            // floats of a head's weights of a unit (padded)
   static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * HEADS * PK * 4, OUT = (size_t)W * HEADS * D * 4,
-                          ZERO = (size_t)W * HEADS * C::NG * 4, STATS = (size_t)W * HEADS * 8;
+                          ZERO = (size_t)W * HEADS * C::NG * 4, STATS = (size_t)(W + 1) * HEADS * 8;
   static constexpr size_t BYTES = RING + WEIGHTS + OUT + ZERO + STATS;
 };
 
@@ -298,21 +298,27 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   constexpr int NG = C::NG, WORDS = D / 32;        // words of a quarter of a row
   const int n = lane >> 2, j = lane & 3;
   const bool second = n >= 4;
-  const uint32_t kc = st, vc = st + C::K_BYTES, ks = st + 2 * C::K_BYTES, kz = ks + D * 4, vs = kz + D * 4, vz = vs + C::UNIT * NG * 4;
+  const uint32_t kc = st, vc = st + C::K_BYTES, ks = st + 2 * C::K_BYTES, vs = ks + 2 * D * 4;
   // --- keys: the queries times the scales of the unit's group in two bf16 terms, and what the zeros and middles give
   uint32_t b[D / 16][2], b2[D / 16][2];              // (kTwo: b alone is multiplied with)
   f32x2 bias = pack2(0.f, 0.f);
   constexpr int MINE = kTwo ? WORDS / 2 : WORDS;
+  // pieces of this lane's quarter: t at t ^ j among four (128 channels; 64: see load_int4)
+  const uint32_t ks_at = ks + (D == 128 ? j * 128 + (kTwo && second ? 64 : 0) : (j >> 1) * 128);
 #pragma unroll
   for (int u = 0; u < MINE; ++u) {
-    const int w = kTwo && second ? u + WORDS / 2 : u;
     float x[8], r[8];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int c = j * (D / 16) + 2 * w + e, at = ((c & ~7) | ((c ^ (c >> 3)) & 7)) * 16;     // 16-byte piece, see load_int4
+      uint32_t at;
+      if constexpr (D == 128) {
+        at = ks_at + ((((2 * u + e) & 3) ^ j) << 4) + ((2 * u + e) >> 2) * 64;
+      } else {
+        at = ks_at + ((((j & 1) * 4 + 2 * (u + (kTwo && second ? WORDS / 2 : 0)) + e) ^ (j >> 1)) << 4);
+      }
       f32x2 sc[2], ze[2];
-      ld_shared2(sc, ks + at);
-      ld_shared2(ze, kz + at);
+      ld_shared(sc, at);
+      ld_shared<D * 4>(ze, at);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const f32x2 q = qf[4 * u + 2 * e + i];
@@ -351,18 +357,12 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   if (kTwo && j >= 2) bias0 = bias1 = 0.f;
   // chains of products that do not wait for one another: two per tile of keys, two for the middles
   float s[2][4], sx[2][4] = {}, mid[4] = {bias0, bias1, bias0, bias1}, midx[4] = {};
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
+  const uint32_t k_at = D == 128 ? kc + n * 64 + ((j ^ ((n >> 1) & 3)) << 4) : kc + n * 32 + j * 8;
+  for_n<2>([&](auto m) {
     s[m][0] = s[m][1] = s[m][2] = s[m][3] = 0.f;
     uint32_t a[WORDS], c[WORDS];
-    const int row = 16 * m + n;
-    if constexpr (D == 128) {
-      ld_shared4(a, kc + row * 64 + ((j ^ ((row >> 1) & 3)) << 4));
-      ld_shared4(c, kc + (row + 8) * 64 + ((j ^ ((row >> 1) & 3)) << 4));
-    } else {
-      ld_shared2u(a, kc + row * 32 + j * 8);
-      ld_shared2u(c, kc + (row + 8) * 32 + j * 8);
-    }
+    ld_shared<m.value * 8 * D>(a, k_at);
+    ld_shared<m.value * 8 * D + 4 * D>(c, k_at);
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       constexpr uint32_t m0 = kMinusMid<0>, m1 = kMinusMid<1>;
@@ -383,7 +383,7 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
         }
       }
     }
-  }
+  });
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -399,27 +399,24 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   for (int half = 0; half < (kTwo ? 1 : 2); ++half) {
     const int kstep = kTwo ? second : half;
     float x[NG][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 16 * kstep + j + 4 * i;
-      const float w = p[row];
+    const uint32_t p_at = smem_addr(p) + (16 * kstep + j) * 4, vs_at = vs + (16 * kstep + j) * NG * 4;
+    for_n<4>([&](auto i) {                           // (zeros lie 32 rows of scales further)
+      const float w = ld_shared_f<i.value * 16>(p_at);
       if constexpr (NG > 1) {
         f32x2 sc[NG / 2], ze[NG / 2];
-        ld_shared_n(sc, vs + row * NG * 4);
-        ld_shared_n(ze, vz + row * NG * 4);
+        ld_shared<i.value * 16 * NG>(sc, vs_at);
+        ld_shared<(i.value * 4 + 32) * NG * 4>(ze, vs_at);
 #pragma unroll
         for (int g = 0; g < NG / 2; ++g) {
           unpack2(mul2(pack2(w, w), sc[g]), x[2 * g][i], x[2 * g + 1][i]);
           R.z[g] = fma2(pack2(w, w), fma2(pack2(8.f, 8.f), sc[g], ze[g]), R.z[g]);
         }
       } else {
-        float sc, ze;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc) : "r"(vs + row * 4) : "memory");
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ze) : "r"(vz + row * 4) : "memory");
+        const float sc = ld_shared_f<i.value * 16>(vs_at), ze = ld_shared_f<(i.value * 4 + 32) * 4>(vs_at);
         x[0][i] = w * sc;
         R.z[0] = fma2(pack2(w, 0.f), pack2(fmaf(8.f, sc, ze), 0.f), R.z[0]);
       }
-    }
+    });
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -434,24 +431,24 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
         }
       }
   }
-#pragma unroll
-  for (int kstep = 0; kstep < 2; ++kstep)
-#pragma unroll
-    for (int blk = 0; blk < D / 32; ++blk) {         // 32 channels: two bytes of this lane's per row
+  // row 16 kstep + j + 4 i, piece blk: at blk ^ (2 (i % 2)) ^ (j / 2) (128 channels)
+  const uint32_t v_at = vc + j * (D / 2) + 2 * n, v_even = v_at + (D == 128 ? (j >> 1) * 16 : 0), v_odd = v_at - (D == 128 ? (j >> 1) * 16 : 0);
+  for_n<2>([&](auto kstep) {
+    for_n<D / 32>([&](auto blk) {                    // 32 channels: two bytes of this lane's per row
       uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 16 * kstep + j + 4 * i, piece = D == 128 ? blk ^ ((row >> 1) & 3) : blk;
-        asm volatile("{\n.reg .u16 t;\nld.shared.u16 t, [%1];\ncvt.u32.u16 %0, t;\n}" : "=r"(h[i]) : "r"(vc + row * (D / 2) + piece * 16 + 2 * n) : "memory");
-      }
+      for_n<4>([&](auto i) {
+        constexpr int piece = D == 128 ? blk.value ^ (2 * (i.value & 1)) : blk.value;
+        h[i] = ld_shared_u16<(16 * kstep.value + 4 * i.value) * (D / 2) + piece * 16>(piece & 1 ? v_odd : v_even);
+      });
       const uint32_t w0 = __byte_perm(h[0], h[1], 0x5410), w1 = __byte_perm(h[2], h[3], 0x5410);
-      constexpr int per = (D / 32) / NG;
-      const int g = blk / per;
-      mma16816(R.o[2 * blk], codes<0>(w0), codes<1>(w0), codes<0>(w1), codes<1>(w1), bb[kstep][g][0], bb[kstep][g][1]);
-      mma16816(R.o[2 * blk + 1], codes<2>(w0), codes<3>(w0), codes<2>(w1), codes<3>(w1), bb[kstep][g][0], bb[kstep][g][1]);
-      mma16816(R.o[2 * blk], kMinusMid<0>, kMinusMid<1>, kMinusMid<0>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
-      mma16816(R.o[2 * blk + 1], kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
-    }
+      constexpr int g = blk.value / ((D / 32) / NG);
+      float (&o0)[4] = R.o[2 * blk], (&o1)[4] = R.o[2 * blk + 1];
+      mma16816(o0, codes<0>(w0), codes<1>(w0), codes<0>(w1), codes<1>(w1), bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(o1, codes<2>(w0), codes<3>(w0), codes<2>(w1), codes<3>(w1), bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(o0, kMinusMid<0>, kMinusMid<1>, kMinusMid<0>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
+      mma16816(o1, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
+    });
+  });
   __syncwarp();
 }
 
@@ -460,11 +457,10 @@ template <int D, int ROWS>
 __device__ __forceinline__ void load_dense(uint32_t dst, const __nv_bfloat16* src, int valid, int lane) {
   constexpr int CH = D / 8, STEP = 32 / CH;
   const int r0 = lane / CH, c = lane % CH;
-#pragma unroll
-  for (int i = 0; i < ROWS / STEP; ++i) {
+  for_n<ROWS / STEP>([&](auto i) {
     const int r = r0 + i * STEP;
-    copy_async16n(dst + (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4)), src + lane * 8 + i * 256, r < valid ? 16 : 0);
-  }
+    copy_async16n<0, i.value * 512>(dst + (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4)), src + lane * 8, r < valid ? 16 : 0);
+  });
 }
 // Copies of a unit of 4-bit rows: codes (128 channels: piece c of a row at c ^ (row / 2 % 4), so that neither the keys' 16-byte
 // nor the values' 2-byte reads meet bank conflicts), the keys' scales and zeros of their group (piece c at c ^ (c / 8) within eight
@@ -475,31 +471,32 @@ __device__ __forceinline__ void load_int4(uint32_t at, const CacheParams& c, int
   constexpr int NG = C::NG, CH = D / 32, ROWS = 32 / CH;                         // pieces of a row; rows of a pass of the warp
   const uint8_t *k = (const uint8_t*)c.k + row * (D / 2) + lane * 16, *v = (const uint8_t*)c.v + row * (D / 2) + lane * 16;
   const int r0 = lane / CH, p = lane % CH;
-#pragma unroll
-  for (int i = 0; i < C::UNIT / ROWS; ++i) {
-    const int r = r0 + i * ROWS;
-    const uint32_t to = at + (uint32_t)(r * (D / 2) + ((D == 128 ? p ^ ((r >> 1) & 3) : p) << 4));
-    const int n = r < valid ? 16 : 0;                                            // beyond: zeros, nothing is read
-    copy_async16n(to, k + i * 512, n);
-    copy_async16n(to + C::K_BYTES, v + i * 512, n);
-  }
+  // (the rows of a lane are 8 or 16 apart: their pieces are turned alike)
+  const uint32_t to = at + (uint32_t)(r0 * (D / 2) + ((D == 128 ? p ^ ((r0 >> 1) & 3) : p) << 4));
+  for_n<C::UNIT / ROWS>([&](auto i) {
+    const int n = r0 + i * ROWS < valid ? 16 : 0;                                // beyond: zeros, nothing is read
+    copy_async16n<i.value * 512, i.value * 512>(to, k, n);
+    copy_async16n<i.value * 512 + C::K_BYTES, i.value * 512>(to, v, n);
+  });
   const uint32_t ks = at + 2 * C::K_BYTES, vs = ks + 2 * C::KS_BYTES;
   if (lane < D / 4) {
-    const int to = ((lane & ~7) | ((lane ^ (lane >> 3)) & 7)) * 16;
-    copy_async16n(ks + to, c.k_scale + kgroup * D + lane * 4, 16);
-    copy_async16n(ks + C::KS_BYTES + to, c.k_zero + kgroup * D + lane * 4, 16);
+    const uint32_t to = ks + ((lane & ~7) | ((lane ^ (lane >> 3)) & 7)) * 16;
+    const int64_t from = kgroup * D + lane * 4;
+    copy_async16n(to, c.k_scale + from, 16);
+    copy_async16n<C::KS_BYTES>(to, c.k_zero + from, 16);
   }
   if constexpr (NG == 4) {                           // a row's scales start on a 16-byte boundary
     const int n = lane < valid ? 16 : 0;
-    copy_async16n(vs + lane * 16, c.v_scale + (row + lane) * 4, n);
-    copy_async16n(vs + C::VS_BYTES + lane * 16, c.v_zero + (row + lane) * 4, n);
+    const int64_t from = (row + lane) * 4;
+    copy_async16n(vs + lane * 16, c.v_scale + from, n);
+    copy_async16n<C::VS_BYTES>(vs + lane * 16, c.v_zero + from, n);
   } else {
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
+    const int64_t from = row * NG + lane;
+    for_n<NG>([&](auto i) {
       const int n = (lane + 32 * i) / NG < valid ? 4 : 0;
-      copy_async4n(vs + (lane + 32 * i) * 4, c.v_scale + row * NG + lane + 32 * i, n);
-      copy_async4n(vs + C::VS_BYTES + (lane + 32 * i) * 4, c.v_zero + row * NG + lane + 32 * i, n);
-    }
+      copy_async4n<i.value * 128, i.value * 128>(vs + lane * 4, c.v_scale + from, n);
+      copy_async4n<i.value * 128 + C::VS_BYTES, i.value * 128>(vs + lane * 4, c.v_zero + from, n);
+    });
   }
 }
 
@@ -514,6 +511,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   float* m_out = (float*)(smem_raw + M::RING + M::WEIGHTS);
   float* m_zero = (float*)(smem_raw + M::RING + M::WEIGHTS + M::OUT);
   float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS + M::OUT + M::ZERO);
+  float2* m_total = m_stat + W * HEADS;
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
   // merge_shares may take its places now; it waits for the end of this kernel before it reads anything of it
@@ -638,23 +636,32 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
       }
     }
     __syncthreads();
+    // every warp's factor to the largest reference of its head (in place of the reference)
+    for (int h = warp; h < G; h += W) {
+      float2 t = lane < W ? m_stat[lane * HEADS + h] : make_float2(-CUDART_INF_F, 0.f);
+      float top = t.x;
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+      const float f = t.y == 0.f ? 0.f : exp2f(t.x - top);      // (a warp without units of this pair)
+      float sum = t.y * f;
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      if (lane < W) m_stat[lane * HEADS + h].x = f;
+      if (lane == 0) m_total[h] = make_float2(top, sum);
+    }
+    __syncthreads();
     const bool whole = work.start >= u0 && work.start + work.units <= u1;
     const int64_t share = (int64_t)blockIdx.x * 2 + (work.start >= u0 ? 1 : 0);
     for (int i = threadIdx.x; i < G * D; i += W * 32) {
       const int h = i / D, ch = i % D;
-      float top = -CUDART_INF_F, sum = 0.f, acc = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) top = fmaxf(top, m_stat[w * HEADS + h].x);
+      float acc = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float2 t = m_stat[w * HEADS + h];
-        if (t.y == 0.f) continue;                    // a warp without units of this pair
-        const float f = exp2f(t.x - top);
         float x = m_out[(w * HEADS + h) * D + ch];
         if constexpr (C::INT4) x += m_zero[(w * HEADS + h) * NG + ch / GROUP];
-        sum = fmaf(t.y, f, sum);
-        acc = fmaf(x, f, acc);
+        acc = fmaf(x, m_stat[w * HEADS + h].x, acc);
       }
+      const float top = m_total[h].x, sum = m_total[h].y;
       if (whole) {
         const int64_t at = (int64_t)work.r * c.Hq + work.g * G + h;
         ((__nv_bfloat16*)c.out)[at * D + ch] = __float2bfloat16_rn(acc / sum);
