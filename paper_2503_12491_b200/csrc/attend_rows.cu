@@ -152,9 +152,10 @@ template <int D, int GROUP, bool kTwo, int W, int ST>
 struct RowsSmem {
   using C = RowsCfg<D, GROUP>;
   static constexpr int HEADS = kTwo ? 4 : 8, PK = 36;                            // floats of a head's weights of a unit (padded)
-  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * HEADS * PK * 4, OUT = (size_t)W * HEADS * D * 4,
-                          ZERO = (size_t)W * HEADS * C::NG * 4, STATS = (size_t)(W + 1) * HEADS * 8;
-  static constexpr size_t BYTES = RING + WEIGHTS + OUT + ZERO + STATS;
+  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * HEADS * PK * 4, STATS = (size_t)(W + 1) * HEADS * 8,
+                          PLACES = (size_t)W * 8, CURSORS = (size_t)W * sizeof(Cursor<D, GROUP>);
+  static constexpr size_t BYTES = RING + WEIGHTS + STATS + PLACES + CURSORS;
+  static_assert(C::STAGE >= HEADS * (D + C::NG) * 4, "a warp's results fit a stage");
 };
 
 // A warp's running softmax: reference and (this lane's part of the) sum of the two heads of its columns 2 j, 2 j + 1, outputs
@@ -355,11 +356,9 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   float bias0 = __shfl_sync(0xffffffffu, bi, 4 * c0), bias1 = __shfl_sync(0xffffffffu, bi, 4 * c0 + 4);
   // with kTwo both terms are added up below, and these must come in once
   if (kTwo && j >= 2) bias0 = bias1 = 0.f;
-  // chains of products that do not wait for one another: two per tile of keys, two for the middles
-  float s[2][4], sx[2][4] = {}, mid[4] = {bias0, bias1, bias0, bias1}, midx[4] = {};
+  float s[2][4] = {}, mid[4] = {bias0, bias1, bias0, bias1};
   const uint32_t k_at = D == 128 ? kc + n * 64 + ((j ^ ((n >> 1) & 3)) << 4) : kc + n * 32 + j * 8;
   for_n<2>([&](auto m) {
-    s[m][0] = s[m][1] = s[m][2] = s[m][3] = 0.f;
     uint32_t a[WORDS], c[WORDS];
     ld_shared<m.value * 8 * D>(a, k_at);
     ld_shared<m.value * 8 * D + 4 * D>(c, k_at);
@@ -369,17 +368,17 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
       const uint32_t a0 = codes<0>(a[w]), a1 = codes<0>(c[w]), a2 = codes<1>(a[w]), a3 = codes<1>(c[w]);
       const uint32_t d0 = codes<2>(a[w]), d1 = codes<2>(c[w]), d2 = codes<3>(a[w]), d3 = codes<3>(c[w]);
       mma16816(s[m], a0, a1, a2, a3, b[2 * w][0], b[2 * w][1]);
-      mma16816(sx[m], d0, d1, d2, d3, b[2 * w + 1][0], b[2 * w + 1][1]);
+      mma16816(s[m], d0, d1, d2, d3, b[2 * w + 1][0], b[2 * w + 1][1]);
       if (m == 0) {
         mma16816(mid, m0, m0, m1, m1, b[2 * w][0], b[2 * w][1]);
-        mma16816(midx, m1, m1, m1, m1, b[2 * w + 1][0], b[2 * w + 1][1]);
+        mma16816(mid, m1, m1, m1, m1, b[2 * w + 1][0], b[2 * w + 1][1]);
       }
       if constexpr (!kTwo) {
         mma16816(s[m], a0, a1, a2, a3, b2[2 * w][0], b2[2 * w][1]);
-        mma16816(sx[m], d0, d1, d2, d3, b2[2 * w + 1][0], b2[2 * w + 1][1]);
+        mma16816(s[m], d0, d1, d2, d3, b2[2 * w + 1][0], b2[2 * w + 1][1]);
         if (m == 0) {
           mma16816(mid, m0, m0, m1, m1, b2[2 * w][0], b2[2 * w][1]);
-          mma16816(midx, m1, m1, m1, m1, b2[2 * w + 1][0], b2[2 * w + 1][1]);
+          mma16816(mid, m1, m1, m1, m1, b2[2 * w + 1][0], b2[2 * w + 1][1]);
         }
       }
     }
@@ -388,7 +387,7 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      s[m][e] = (s[m][e] + sx[m][e]) + (mid[e] + midx[e]);
+      s[m][e] += mid[e];
       if (kTwo) s[m][e] += __shfl_xor_sync(0xffffffffu, s[m][e], 2);
     }
   weigh<D, NG, kTwo, 2, PK>(R, s, valid, scale2, sp, lane);
@@ -508,10 +507,10 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* ring = smem_raw;
   float* weights = (float*)(smem_raw + M::RING);
-  float* m_out = (float*)(smem_raw + M::RING + M::WEIGHTS);
-  float* m_zero = (float*)(smem_raw + M::RING + M::WEIGHTS + M::OUT);
-  float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS + M::OUT + M::ZERO);
+  float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS);
   float2* m_total = m_stat + W * HEADS;
+  int* m_place = (int*)(smem_raw + M::RING + M::WEIGHTS + M::STATS);             // where a warp's results lie in the ring
+  Cursor<D, GROUP>* cursors = (Cursor<D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS + M::STATS + M::PLACES);
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
   // merge_shares may take its places now; it waits for the end of this kernel before it reads anything of it
@@ -523,15 +522,24 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   const int total = Q.all * c.Hkv, per = per_cta(total, gridDim.x);
   const int u0 = (int)min((int64_t)total, (int64_t)blockIdx.x * per), u1 = min(u0 + per, total);
   if (u0 >= u1) return;
-  Cursor<D, GROUP> load, work;
-  load.open(c, P.n_req, Q, u0, lane);
-  work = load;
+  Cursor<D, GROUP> work;
+  work.open(c, P.n_req, Q, u0, lane);
+  // the place of the copies, which run ahead, lies in shared memory: it is read once per unit, registers are short
+  Cursor<D, GROUP>& load = cursors[warp];
+  if (lane == 0) load = work;
+  __syncwarp();
 
   uint8_t* my_ring = ring + (size_t)warp * ST * C::STAGE;
   auto issue = [&](int k) {                          // copies of this warp's k-th unit
     const int u = u0 + warp + k * W;
     if (u < u1) {
-      load.seek(c, P.n_req, u);
+      if (u - load.start >= load.units) {
+        Cursor<D, GROUP> to = load;
+        to.seek(c, P.n_req, u);
+        __syncwarp();
+        if (lane == 0) load = to;
+        __syncwarp();
+      }
       const int packed = (int)((load.len.n + C::UNIT - 1) / C::UNIT), at = u - load.start;
       uint8_t* st = my_ring + (size_t)(k % ST) * C::STAGE;
       if (at < packed) {
@@ -567,7 +575,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     // the queries of this lane's column, as the products take them
     const __nv_bfloat16* q = (const __nv_bfloat16*)c.q + ((int64_t)work.r * c.Hq + work.g * G + head) * D;
     const bool live = head < G;
-    uint32_t qd[D / 16][2];
+    uint32_t qd[C::INT4 ? 1 : D / 16][2];
     constexpr int QW = D / (kTwo ? 64 : 32);         // pieces of eight channels
     f32x2 qf[C::INT4 ? 4 * QW : 1];
     if constexpr (C::INT4) {
@@ -580,13 +588,14 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         qf[4 * i + 3] = pack2(__uint_as_float(w.w << 16), __uint_as_float(w.w & 0xFFFF0000u));
       }
     }
-    if (!C::INT4 || work.len.tail > 0) {
+    auto dense_queries = [&](uint32_t (&x)[D / 16][2]) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        qd[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
-        qd[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
+        x[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
+        x[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
       }
-    }
+    };
+    if constexpr (!C::INT4) dense_queries(qd);
     for (; u0 + warp + k * W < end; ++k) {
       issue(k + ST - 1);
       copy_wait<ST - 1>();
@@ -599,10 +608,20 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         else dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::K_BYTES, valid, c.scale2, sp, lane);
       } else {
         const int valid = min(C::TAIL, work.len.tail - (at - packed) * C::TAIL);
-        dense_unit<D, NG, kTwo, C::TAIL == 32 ? 2 : 1, PK>(R, qd, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
+        if constexpr (C::INT4) {                     // few rows: their queries are read again rather than kept
+          uint32_t x[D / 16][2];
+          dense_queries(x);
+          dense_unit<D, NG, kTwo, 1, PK>(R, x, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
+        } else {
+          dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
+        }
       }
     }
-    // --- the pair ends here (or this CTA's part of it): the warps' results together
+    // --- the pair ends here (or this CTA's part of it): the warps' results together, each in the one stage of its ring that
+    // holds no unit to come
+    const int place = (warp * ST + (k + ST - 1) % ST) * C::STAGE;
+    float *m_out = (float*)(ring + place), *m_zero = m_out + HEADS * D;
+    if (lane == 0) m_place[warp] = place;
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) {
       R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
@@ -620,7 +639,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
       for (int e = 0; e < 4; ++e) {
         float x = R.o[i][e];
         if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 2);
-        if (!kTwo || j < 2) m_out[(warp * HEADS + 2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
+        if (!kTwo || j < 2) m_out[(2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
       }
     }
     if constexpr (C::INT4) {
@@ -632,7 +651,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         x += __shfl_xor_sync(0xffffffffu, x, 1);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 16);
-        if (j == 0 && (!kTwo || n < 4)) m_zero[(warp * HEADS + head) * NG + i] = x;
+        if (j == 0 && (!kTwo || n < 4)) m_zero[head * NG + i] = x;
       }
     }
     __syncthreads();
@@ -657,8 +676,9 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
       float acc = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        float x = m_out[(w * HEADS + h) * D + ch];
-        if constexpr (C::INT4) x += m_zero[(w * HEADS + h) * NG + ch / GROUP];
+        const float* of = (const float*)(ring + m_place[w]);
+        float x = of[h * D + ch];
+        if constexpr (C::INT4) x += of[HEADS * D + h * NG + ch / GROUP];
         acc = fmaf(x, m_stat[w * HEADS + h].x, acc);
       }
       const float top = m_total[h].x, sum = m_total[h].y;
@@ -797,7 +817,8 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
 
 template <int D, int GROUP>
 cudaError_t run_rows(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
-  // Warps and stages as shared memory holds them: bf16 rows 4 x 3 stages of 8 to 16 KB, 4-bit rows 12 x 2 of 2 to 6 KB.
+  // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, 4-bit rows 12 x 2 of 2 to
+  // 6 KB (8 warps are as fast, 16 slower by 8 %: they have no more than 128 registers each).
   constexpr int W = GROUP ? 12 : 4, ST = GROUP ? 2 : 3;
   return P.c.Hq / P.c.Hkv <= 4 ? run_units<D, GROUP, true, W, ST>(ctx, P, st) : run_units<D, GROUP, false, W, ST>(ctx, P, st);
 }
