@@ -1,23 +1,26 @@
-// Attention of one new token per request over its cached rows, bf16 queries: the rows in bf16 or in 4 bits.
+// Attention of one new token per request over its cached rows: the rows in the context's type (bf16 or fp32) or in 4 bits, and behind
+// either the rows of tokens generated since.
+//
+//   O_h = sum_j softmax_j(q_h.k_j / sqrt d) v_j ,  lse_h = log sum_j exp(q_h.k_j / sqrt d)   over all rows j of h's KV head.
 #include "cache_mma.cuh"
 #include "tc_ptx.cuh"
 
 namespace cake {
 namespace {
 
-// ------------------------------------------------------------------ bf16 and 4-bit rows on the tensor cores
+//
 // Work.  The (request, KV head) pairs of the layer are cut into units of 32 rows (the tail's rows behind the packed ones; 8 rows
 // a unit in the 4-bit kernel, whose stages are smaller), and every CTA of one per SM takes the same number of consecutive
 // units, whatever pairs they belong to: the device works evenly on ragged batches, and on one long request.  Lengths lie on
 // the device, so each CTA adds up the units of all requests for itself.  Inside a CTA the warps take the units in turn, each
 // with copies of its own units in flight (cp.async) and its own running softmax; they meet only where a pair ends.  A pair that
 // lies in one CTA is finished there; of the others a CTA leaves its share in the workspace (at most one share at either end
-// of its run), and merge_shares, which is already resident when the last CTA ends, puts them together.
+// of its run), and merge_shares, which waits for the last CTA on its SMs, puts them together.
 //
-// Products (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the query heads as the 8 columns.  With
+// bf16 queries: products on the tensor cores (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the query heads as the 8 columns.  With
 // up to four heads the columns 4 to 7 hold the same heads once more, for the second term of what is held in two bf16 terms
-// (kTwo): the weights of bf16 rows, and queries times scales, are then exact to 2^-16.  With more heads the 4-bit kernel
-// multiplies the keys twice; weights are rounded to bf16, and so are, with any number of heads, weights times scales.
+// (kTwo): weights, and queries and weights times scales, are then exact to 2^-16.  With more heads the 4-bit kernel
+// multiplies twice, and the weights of bf16 rows are rounded to bf16.
 //
 // 4-bit rows.  A code c becomes the bf16 16 + c (or 128 + c) by a logical operation per pair and at most one shift; scales and
 // zeros are never applied to a row but to the other operand: q_c s_c for the keys, p_j s_j for the values, and
@@ -28,14 +31,14 @@ namespace {
 // channels come from one group of 32, which has one scale per row.
 constexpr float kRefSlack = 8.f;                 // powers of two a maximum may lie above the reference before all is rescaled
 
-template <int D, int GROUP> struct RowsCfg {
-  static constexpr bool INT4 = GROUP != 0;
-  static constexpr int UNIT = 32, TAIL = INT4 ? 8 : 32;                          // rows of a unit
+template <typename T, int D, int GROUP> struct RowsCfg {
+  static constexpr bool INT4 = GROUP != 0, F32 = sizeof(T) == 4;
+  static constexpr int UNIT = 32, TAIL = !INT4 ? 32 : F32 ? 4 : 8;               // rows of a unit
   static constexpr int NG = INT4 ? D / GROUP : 1;                                // channel groups of a row
-  static constexpr int K_BYTES = INT4 ? UNIT * D / 2 : UNIT * D * 2;
+  static constexpr int K_BYTES = INT4 ? UNIT * D / 2 : UNIT * D * (int)sizeof(T);
   static constexpr int VS_BYTES = INT4 ? UNIT * NG * 4 : 0, KS_BYTES = INT4 ? D * 4 : 0;
   static constexpr int STAGE = 2 * (K_BYTES + VS_BYTES + KS_BYTES);
-  static_assert(!INT4 || TAIL * D * 4 <= STAGE, "tail rows fit a stage");
+  static_assert(2 * TAIL * D * (int)sizeof(T) <= STAGE, "tail rows fit a stage");
 };
 
 struct RowsParams {
@@ -101,9 +104,9 @@ struct Requests {
 __device__ __forceinline__ int per_cta(int units, int ctas) { return max(1, (units + ctas - 1) / ctas); }
 
 // A place in the sequence of units: moves forward only.
-template <int D, int GROUP>
+template <typename T, int D, int GROUP>
 struct Cursor {
-  using C = RowsCfg<D, GROUP>;
+  using C = RowsCfg<T, D, GROUP>;
   int r, g;
   int start, units;                              // first unit of the pair, and how many it has
   Lengths len;
@@ -142,18 +145,21 @@ struct Cursor {
   __device__ __forceinline__ void seek(const CacheParams& c, int n_req, int u) { while (u - start >= units) next(c, n_req); }
 };
 
+__device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
+__device__ __forceinline__ void narrow(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
 __device__ __forceinline__ float ex2a(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-template <int D, int GROUP, bool kTwo, int W, int ST>
+template <typename T, int D, int GROUP, bool kTwo, int W, int ST>
 struct RowsSmem {
-  using C = RowsCfg<D, GROUP>;
+  using C = RowsCfg<T, D, GROUP>;
   static constexpr int HEADS = kTwo ? 4 : 8, PK = 36;                            // floats of a head's weights of a unit (padded)
-  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * HEADS * PK * 4, STATS = (size_t)(W + 1) * HEADS * 8,
-                          PLACES = (size_t)W * 8, CURSORS = (size_t)W * sizeof(Cursor<D, GROUP>);
+  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * (HEADS * PK + (C::F32 ? HEADS * D : 0)) * 4, STATS = (size_t)(W + 1) * HEADS * 8,
+                          PLACES = (size_t)W * 8, CURSORS = (size_t)W * sizeof(Cursor<T, D, GROUP>);
   static constexpr size_t BYTES = RING + WEIGHTS + STATS + PLACES + CURSORS;
   static_assert(C::STAGE >= HEADS * (D + C::NG) * 4, "a warp's results fit a stage");
 };
@@ -295,7 +301,7 @@ template <int I> constexpr uint32_t kMinusMid = I == 0 ? 0xC308C308u : 0xC1C0C1C
 template <int D, int GROUP, bool kTwo, int PK>
 __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 (&qf)[D / (kTwo ? 16 : 8)], uint32_t st, int valid, float scale2, float* sp,
                                           int lane) {
-  using C = RowsCfg<D, GROUP>;
+  using C = RowsCfg<__nv_bfloat16, D, GROUP>;
   constexpr int NG = C::NG, WORDS = D / 32;        // words of a quarter of a row
   const int n = lane >> 2, j = lane & 3;
   const bool second = n >= 4;
@@ -393,7 +399,7 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
   weigh<D, NG, kTwo, 2, PK>(R, s, valid, scale2, sp, lane);
   // --- values: keys j, j + 4, j + 8, j + 12 of 16; the weights times the scales
   const float* p = sp + (kTwo ? n & 3 : n) * PK;
-  uint32_t bb[2][NG][2];
+  uint32_t bb[2][NG][2], b3[2][NG][2];               // leading terms and the rest (kTwo: as this lane's column takes them, in bb)
 #pragma unroll
   for (int half = 0; half < (kTwo ? 1 : 2); ++half) {
     const int kstep = kTwo ? second : half;
@@ -420,13 +426,15 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint32_t v = bf16_pair(x[g][2 * u], x[g][2 * u + 1]);
+        const float a = bf16_floor(x[g][2 * u]), b = bf16_floor(x[g][2 * u + 1]);
+        const uint32_t lead = bf16_pair(a, b), rest = bf16_pair(x[g][2 * u] - a, x[g][2 * u + 1] - b);
         if constexpr (kTwo) {
-          const uint32_t got = __shfl_xor_sync(0xffffffffu, v, 16);             // the columns from 4 on stay empty
-          bb[0][g][u] = second ? 0u : v;
-          bb[1][g][u] = second ? 0u : got;
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, second ? lead : rest, 16);
+          bb[0][g][u] = second ? got : lead;
+          bb[1][g][u] = second ? rest : got;
         } else {
-          bb[half][g][u] = v;
+          bb[half][g][u] = lead;
+          b3[half][g][u] = rest;
         }
       }
   }
@@ -446,19 +454,27 @@ __device__ __forceinline__ void int4_unit(Running<D, D / GROUP>& R, const f32x2 
       mma16816(o1, codes<2>(w0), codes<3>(w0), codes<2>(w1), codes<3>(w1), bb[kstep][g][0], bb[kstep][g][1]);
       mma16816(o0, kMinusMid<0>, kMinusMid<1>, kMinusMid<0>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
       mma16816(o1, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, bb[kstep][g][0], bb[kstep][g][1]);
+      if constexpr (!kTwo) {
+        mma16816(o0, codes<0>(w0), codes<1>(w0), codes<0>(w1), codes<1>(w1), b3[kstep][g][0], b3[kstep][g][1]);
+        mma16816(o1, codes<2>(w0), codes<3>(w0), codes<2>(w1), codes<3>(w1), b3[kstep][g][0], b3[kstep][g][1]);
+        mma16816(o0, kMinusMid<0>, kMinusMid<1>, kMinusMid<0>, kMinusMid<1>, b3[kstep][g][0], b3[kstep][g][1]);
+        mma16816(o1, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, kMinusMid<1>, b3[kstep][g][0], b3[kstep][g][1]);
+      }
     });
   });
   __syncwarp();
 }
 
-// Copies of `rows` bf16 rows (those from `valid` on read as zeros) into shared memory, 16-byte piece c of a row at c ^ (row % 8).
-template <int D, int ROWS>
-__device__ __forceinline__ void load_dense(uint32_t dst, const __nv_bfloat16* src, int valid, int lane) {
-  constexpr int CH = D / 8, STEP = 32 / CH;
+// Copies of ROWS rows of the context's type (those from `valid` on read as zeros) into shared memory, 16-byte piece c of a row at
+// c ^ (row % 8).
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void load_dense(uint32_t dst, const T* src, int valid, int lane) {
+  constexpr int CH = D * (int)sizeof(T) / 16, STEP = 32 / CH;
   const int r0 = lane / CH, c = lane % CH;
   for_n<ROWS / STEP>([&](auto i) {
     const int r = r0 + i * STEP;
-    copy_async16n<0, i.value * 512>(dst + (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4)), src + lane * 8, r < valid ? 16 : 0);
+    copy_async16n<0, i.value * 512>(dst + (uint32_t)(r * D * (int)sizeof(T) + ((c ^ (r & 7)) << 4)), (const uint8_t*)src + lane * 16,
+                                    r < valid ? 16 : 0);
   });
 }
 // Copies of a unit of 4-bit rows: codes (128 channels: piece c of a row at c ^ (row / 2 % 4), so that neither the keys' 16-byte
@@ -466,7 +482,7 @@ __device__ __forceinline__ void load_dense(uint32_t dst, const __nv_bfloat16* sr
 // pieces, for the same reason), the values' scales and zeros.
 template <int D, int GROUP>
 __device__ __forceinline__ void load_int4(uint32_t at, const CacheParams& c, int64_t row, int64_t kgroup, int valid, int lane) {
-  using C = RowsCfg<D, GROUP>;
+  using C = RowsCfg<float, D, GROUP>;                // (4-bit rows lie in shared memory alike for both types)
   constexpr int NG = C::NG, CH = D / 32, ROWS = 32 / CH;                         // pieces of a row; rows of a pass of the warp
   const uint8_t *k = (const uint8_t*)c.k + row * (D / 2) + lane * 16, *v = (const uint8_t*)c.v + row * (D / 2) + lane * 16;
   const int r0 = lane / CH, p = lane % CH;
@@ -499,10 +515,153 @@ __device__ __forceinline__ void load_int4(uint32_t at, const CacheParams& c, int
   }
 }
 
-template <int D, int GROUP, bool kTwo, int W, int ST>
+// ------------------------------------------------------------------ fp32 queries
+// Products in fp32 FMA.  For the logits a lane is a key, for the outputs it owns D / 32 channels: the keys' weights go through
+// shared memory in between, and the queries come from there too, as 16-byte pieces that all lanes read at once.
+template <int D, int HEADS>
+struct Running32 {
+  float ref[HEADS], sum[HEADS], o[HEADS][D / 32];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      ref[h] = -CUDART_INF_F;
+      sum[h] = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[h][c] = 0.f;
+    }
+  }
+};
+// Weights of a unit's keys (this lane's: s) into shared memory as [key][head].
+template <int D, int HEADS>
+__device__ __forceinline__ void weigh32(Running32<D, HEADS>& R, float (&s)[HEADS], int valid, float scale2, float* sp, int lane) {
+#pragma unroll
+  for (int h = 0; h < HEADS; ++h) {
+    s[h] = lane < valid ? s[h] * scale2 : -CUDART_INF_F;
+    float top = s[h];
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    if (top > R.ref[h] + kRefSlack) {                // (the whole warp has the same values)
+      const float f = exp2f(R.ref[h] - top);
+      R.ref[h] = top;
+      R.sum[h] *= f;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) R.o[h][c] *= f;
+    }
+    const float p = exp2f(s[h] - R.ref[h]);
+    R.sum[h] += p;                                   // of this lane's keys
+    sp[lane * HEADS + h] = p;
+  }
+  __syncwarp();
+}
+// v: this lane's channels of key `j`.
+template <int D, int HEADS>
+__device__ __forceinline__ void add_row(Running32<D, HEADS>& R, const float* sp, int j, const float (&v)[D / 32]) {
+#pragma unroll
+  for (int h = 0; h < HEADS; h += 4) {
+    const float4 p = *reinterpret_cast<const float4*>(sp + j * HEADS + h);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      R.o[h][c] = fmaf(p.x, v[c], R.o[h][c]);
+      R.o[h + 1][c] = fmaf(p.y, v[c], R.o[h + 1][c]);
+      R.o[h + 2][c] = fmaf(p.z, v[c], R.o[h + 2][c]);
+      R.o[h + 3][c] = fmaf(p.w, v[c], R.o[h + 3][c]);
+    }
+  }
+}
+// ROWS rows in fp32; qs: queries [head][channel].
+template <int D, int HEADS, int ROWS>
+__device__ __forceinline__ void dense32_unit(Running32<D, HEADS>& R, const float* qs, const uint8_t* k, const uint8_t* v, int valid, float scale2,
+                                             float* sp, int lane) {
+  const int row = min(lane, ROWS - 1);
+  float s[HEADS] = {};
+#pragma unroll 4
+  for (int c = 0; c < D / 4; ++c) {
+    const float4 x = *reinterpret_cast<const float4*>(k + row * D * 4 + ((c ^ (row & 7)) << 4));
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      const float4 q = *reinterpret_cast<const float4*>(qs + h * D + 4 * c);
+      s[h] = fmaf(q.x, x.x, fmaf(q.y, x.y, fmaf(q.z, x.z, fmaf(q.w, x.w, s[h]))));
+    }
+  }
+  weigh32<D, HEADS>(R, s, valid, scale2, sp, lane);
+#pragma unroll 4
+  for (int j = 0; j < min(valid, ROWS); ++j) {
+    float x[D / 32];
+    if constexpr (D == 128) {
+      const float4 y = *reinterpret_cast<const float4*>(v + j * 512 + ((lane ^ (j & 7)) << 4));
+      x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+    } else {
+      const float2 y = *reinterpret_cast<const float2*>(v + j * 256 + (((lane >> 1) ^ (j & 7)) << 4) + (lane & 1) * 8);
+      x[0] = y.x; x[1] = y.y;
+    }
+    add_row<D, HEADS>(R, sp, j, x);
+  }
+  __syncwarp();
+}
+// 16 + code of the nibble at bit 4 i, in fp32 (the mantissa's upper four bits).
+__device__ __forceinline__ float code32(uint32_t w, int i) {
+  return __uint_as_float(((4 * i < 19 ? w << (19 - 4 * i) : w >> (4 * i - 19)) & 0x00780000u) | 0x41800000u);
+}
+// 32 rows in 4 bits, in the layout of load_int4; q: this lane's channels of the queries, qs: room for them times the unit's scales.
+template <int D, int GROUP, int HEADS>
+__device__ __forceinline__ void int4_unit32(Running32<D, HEADS>& R, const float (&q)[HEADS][D / 32], float* qs, const uint8_t* st, int valid,
+                                            float scale2, float* sp, int lane) {
+  using C = RowsCfg<float, D, GROUP>;
+  constexpr int NG = C::NG, CL = D / 32;
+  const uint8_t *kc = st, *vc = st + C::K_BYTES;
+  const float *ks = (const float*)(st + 2 * C::K_BYTES), *kz = ks + D, *vs = kz + D, *vz = vs + C::UNIT * NG;
+  const int piece = lane * CL / 4, at = ((piece & ~7) | ((piece ^ (piece >> 3)) & 7)) * 4 + (lane * CL & 3);
+  float s[HEADS];
+#pragma unroll
+  for (int h = 0; h < HEADS; ++h) {
+    s[h] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CL; ++c) {
+      const float sc = ks[at + c];
+      qs[h * D + lane * CL + c] = q[h][c] * sc;
+      s[h] = fmaf(q[h][c], fmaf(-16.f, sc, kz[at + c]), s[h]);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) s[h] += __shfl_xor_sync(0xffffffffu, s[h], x);
+  }
+  __syncwarp();
+#pragma unroll
+  for (int p = 0; p < D / 32; ++p) {                 // 32 channels of this lane's key
+    const uint4 w4 = *reinterpret_cast<const uint4*>(kc + lane * (D / 2) + ((D == 128 ? p ^ ((lane >> 1) & 3) : p) << 4));
+    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = code32(w[e], i);
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) {
+        const float4 a = *reinterpret_cast<const float4*>(qs + h * D + 32 * p + 8 * e), b = *reinterpret_cast<const float4*>(qs + h * D + 32 * p + 8 * e + 4);
+        s[h] = fmaf(a.x, x[0], fmaf(a.y, x[1], fmaf(a.z, x[2], fmaf(a.w, x[3], s[h]))));
+        s[h] = fmaf(b.x, x[4], fmaf(b.y, x[5], fmaf(b.z, x[6], fmaf(b.w, x[7], s[h]))));
+      }
+    }
+  }
+  weigh32<D, HEADS>(R, s, valid, scale2, sp, lane);
+  const int g = lane * CL / GROUP;
+#pragma unroll 4
+  for (int j = 0; j < valid; ++j) {
+    const float sc = vs[j * NG + g], ze = fmaf(-16.f, sc, vz[j * NG + g]);
+    float x[CL];
+    const int byte = lane * CL / 2, from = j * (D / 2) + ((D == 128 ? (byte >> 4) ^ ((j >> 1) & 3) : byte >> 4) << 4) + (byte & 15);
+    const uint32_t w = CL == 4 ? *reinterpret_cast<const uint16_t*>(vc + from) : vc[from];
+#pragma unroll
+    for (int c = 0; c < CL; ++c) x[c] = fmaf(code32(w, c), sc, ze);
+    add_row<D, HEADS>(R, sp, j, x);
+  }
+  __syncwarp();
+}
+
+// ------------------------------------------------------------------ the kernel
+template <typename T, int D, int GROUP, bool kTwo, int W, int ST>
 __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
-  using C = RowsCfg<D, GROUP>;
-  using M = RowsSmem<D, GROUP, kTwo, W, ST>;
+  using C = RowsCfg<T, D, GROUP>;
+  using M = RowsSmem<T, D, GROUP, kTwo, W, ST>;
   constexpr int HEADS = M::HEADS, NG = C::NG, PK = M::PK;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* ring = smem_raw;
@@ -510,7 +669,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS);
   float2* m_total = m_stat + W * HEADS;
   int* m_place = (int*)(smem_raw + M::RING + M::WEIGHTS + M::STATS);             // where a warp's results lie in the ring
-  Cursor<D, GROUP>* cursors = (Cursor<D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS + M::STATS + M::PLACES);
+  Cursor<T, D, GROUP>* cursors = (Cursor<T, D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS + M::STATS + M::PLACES);
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
   // merge_shares may take its places now; it waits for the end of this kernel before it reads anything of it
@@ -522,10 +681,10 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   const int total = Q.all * c.Hkv, per = per_cta(total, gridDim.x);
   const int u0 = (int)min((int64_t)total, (int64_t)blockIdx.x * per), u1 = min(u0 + per, total);
   if (u0 >= u1) return;
-  Cursor<D, GROUP> work;
+  Cursor<T, D, GROUP> work;
   work.open(c, P.n_req, Q, u0, lane);
   // the place of the copies, which run ahead, lies in shared memory: it is read once per unit, registers are short
-  Cursor<D, GROUP>& load = cursors[warp];
+  Cursor<T, D, GROUP>& load = cursors[warp];
   if (lane == 0) load = work;
   __syncwarp();
 
@@ -534,7 +693,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     const int u = u0 + warp + k * W;
     if (u < u1) {
       if (u - load.start >= load.units) {
-        Cursor<D, GROUP> to = load;
+        Cursor<T, D, GROUP> to = load;
         to.seek(c, P.n_req, u);
         __syncwarp();
         if (lane == 0) load = to;
@@ -549,14 +708,14 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           load_int4<D, GROUP>(smem_addr(st), c, row, load.len.kgroup + load.g * ((load.len.n + GROUP - 1) / GROUP) + (int64_t)at * C::UNIT / GROUP,
                               valid, lane);
         } else {
-          load_dense<D, C::UNIT>(smem_addr(st), (const __nv_bfloat16*)c.k + row * D, valid, lane);
-          load_dense<D, C::UNIT>(smem_addr(st) + C::K_BYTES, (const __nv_bfloat16*)c.v + row * D, valid, lane);
+          load_dense<T, D, C::UNIT>(smem_addr(st), (const T*)c.k + row * D, valid, lane);
+          load_dense<T, D, C::UNIT>(smem_addr(st) + C::K_BYTES, (const T*)c.v + row * D, valid, lane);
         }
       } else {
         const int t0 = (at - packed) * C::TAIL, valid = min(C::TAIL, load.len.tail - t0);
         const int64_t row = ((int64_t)load.r * c.Hkv + load.g) * c.tail_cap + t0;
-        load_dense<D, C::TAIL>(smem_addr(st), (const __nv_bfloat16*)c.k_tail + row * D, valid, lane);
-        load_dense<D, C::TAIL>(smem_addr(st) + C::TAIL * D * 2, (const __nv_bfloat16*)c.v_tail + row * D, valid, lane);
+        load_dense<T, D, C::TAIL>(smem_addr(st), (const T*)c.k_tail + row * D, valid, lane);
+        load_dense<T, D, C::TAIL>(smem_addr(st) + C::TAIL * D * (int)sizeof(T), (const T*)c.v_tail + row * D, valid, lane);
       }
     }
     copy_commit();
@@ -566,92 +725,144 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
 
   const int n = lane >> 2, j = lane & 3, head = kTwo ? n & 3 : n;
   float* sp = weights + warp * HEADS * PK;
+  float* qs = weights + W * HEADS * PK + warp * HEADS * D;                       // (fp32: queries)
   int k = 0;
   for (int u = u0; u < u1; ) {                   // pair by pair
     work.seek(c, P.n_req, u);
     const int end = min(work.start + work.units, u1), packed = (int)((work.len.n + C::UNIT - 1) / C::UNIT);
-    Running<D, NG> R;
-    R.clear();
-    // the queries of this lane's column, as the products take them
-    const __nv_bfloat16* q = (const __nv_bfloat16*)c.q + ((int64_t)work.r * c.Hq + work.g * G + head) * D;
-    const bool live = head < G;
-    uint32_t qd[C::INT4 ? 1 : D / 16][2];
-    constexpr int QW = D / (kTwo ? 64 : 32);         // pieces of eight channels
-    f32x2 qf[C::INT4 ? 4 * QW : 1];
-    if constexpr (C::INT4) {
-#pragma unroll
-      for (int i = 0; i < QW; ++i) {
-        const uint4 w = live ? *reinterpret_cast<const uint4*>(q + j * (D / 4) + 8 * (i + (kTwo && n >= 4 ? QW : 0))) : make_uint4(0, 0, 0, 0);
-        qf[4 * i] = pack2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u));
-        qf[4 * i + 1] = pack2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
-        qf[4 * i + 2] = pack2(__uint_as_float(w.z << 16), __uint_as_float(w.z & 0xFFFF0000u));
-        qf[4 * i + 3] = pack2(__uint_as_float(w.w << 16), __uint_as_float(w.w & 0xFFFF0000u));
-      }
-    }
-    auto dense_queries = [&](uint32_t (&x)[D / 16][2]) {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        x[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
-        x[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
-      }
-    };
-    if constexpr (!C::INT4) dense_queries(qd);
-    for (; u0 + warp + k * W < end; ++k) {
-      issue(k + ST - 1);
-      copy_wait<ST - 1>();
-      __syncwarp();
-      const int at = u0 + warp + k * W - work.start;
-      uint8_t* st = my_ring + (size_t)(k % ST) * C::STAGE;
-      if (at < packed) {
-        const int valid = (int)min((int64_t)C::UNIT, work.len.n - (int64_t)at * C::UNIT);
-        if constexpr (C::INT4) int4_unit<D, GROUP, kTwo, PK>(R, qf, smem_addr(st), valid, c.scale2, sp, lane);
-        else dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::K_BYTES, valid, c.scale2, sp, lane);
-      } else {
-        const int valid = min(C::TAIL, work.len.tail - (at - packed) * C::TAIL);
-        if constexpr (C::INT4) {                     // few rows: their queries are read again rather than kept
-          uint32_t x[D / 16][2];
-          dense_queries(x);
-          dense_unit<D, NG, kTwo, 1, PK>(R, x, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
-        } else {
-          dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
-        }
-      }
-    }
     // --- the pair ends here (or this CTA's part of it): the warps' results together, each in the one stage of its ring that
     // holds no unit to come
-    const int place = (warp * ST + (k + ST - 1) % ST) * C::STAGE;
-    float *m_out = (float*)(ring + place), *m_zero = m_out + HEADS * D;
-    if (lane == 0) m_place[warp] = place;
+    int place;
+    float* m_out;
+    auto open_place = [&]() {
+      place = (warp * ST + (k + ST - 1) % ST) * C::STAGE;
+      m_out = (float*)(ring + place);
+      if (lane == 0) m_place[warp] = place;
+    };
+    if constexpr (C::F32) {
+      Running32<D, HEADS> R;
+      R.clear();
+      const float* q = (const float*)c.q + ((int64_t)work.r * c.Hq + work.g * G) * D;
+      float qr[HEADS][D / 32];                       // this lane's channels
 #pragma unroll
-    for (int x = 4; x < 32; x <<= 1) {
-      R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
-      R.sum[1] += __shfl_xor_sync(0xffffffffu, R.sum[1], x);
-    }
-    if (n == 0 && (!kTwo || j < 2)) {
-      m_stat[warp * HEADS + 2 * j] = make_float2(R.ref[0], R.sum[0]);
-      m_stat[warp * HEADS + 2 * j + 1] = make_float2(R.ref[1], R.sum[1]);
-    }
+      for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      // channels of the tile's rows lane / 4 and + 8
-      const int ch0 = C::INT4 ? 32 * (i / 2) + 4 * n + 2 * (i & 1) : 16 * i + n, ch1 = C::INT4 ? ch0 + 1 : ch0 + 8;
+        for (int i = 0; i < D / 32; ++i) {
+          qr[h][i] = h < G ? q[h * D + lane * (D / 32) + i] : 0.f;
+          if (!C::INT4) qs[h * D + lane * (D / 32) + i] = qr[h][i];
+        }
+      __syncwarp();
+      for (; u0 + warp + k * W < end; ++k) {
+        issue(k + ST - 1);
+        copy_wait<ST - 1>();
+        __syncwarp();
+        const int at = u0 + warp + k * W - work.start;
+        uint8_t* st = my_ring + (size_t)(k % ST) * C::STAGE;
+        if (at < packed) {
+          const int valid = (int)min((int64_t)C::UNIT, work.len.n - (int64_t)at * C::UNIT);
+          if constexpr (C::INT4) int4_unit32<D, GROUP, HEADS>(R, qr, qs, st, valid, c.scale2, sp, lane);
+          else dense32_unit<D, HEADS, C::UNIT>(R, qs, st, st + C::K_BYTES, valid, c.scale2, sp, lane);
+        } else {
+          const int valid = min(C::TAIL, work.len.tail - (at - packed) * C::TAIL);
+          if constexpr (C::INT4) {                   // (the room for the queries holds them times some unit's scales)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = R.o[i][e];
-        if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 2);
-        if (!kTwo || j < 2) m_out[(2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
+            for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+              for (int i = 0; i < D / 32; ++i) qs[h * D + lane * (D / 32) + i] = qr[h][i];
+            __syncwarp();
+          }
+          dense32_unit<D, HEADS, C::TAIL>(R, qs, st, st + C::TAIL * D * 4, valid, c.scale2, sp, lane);
+        }
       }
-    }
-    if constexpr (C::INT4) {
+      open_place();
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        float x, y;
-        unpack2(R.z[i / 2], x, y);
-        if (i & 1) x = y;
-        x += __shfl_xor_sync(0xffffffffu, x, 1);
-        x += __shfl_xor_sync(0xffffffffu, x, 2);
-        if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 16);
-        if (j == 0 && (!kTwo || n < 4)) m_zero[head * NG + i] = x;
+      for (int h = 0; h < HEADS; ++h) {
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) R.sum[h] += __shfl_xor_sync(0xffffffffu, R.sum[h], x);
+        if (lane == 0) m_stat[warp * HEADS + h] = make_float2(R.ref[h], R.sum[h]);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) m_out[h * D + lane * (D / 32) + i] = R.o[h][i];
+      }
+    } else {
+      Running<D, NG> R;
+      R.clear();
+      // the queries of this lane's column, as the products take them
+      const __nv_bfloat16* q = (const __nv_bfloat16*)c.q + ((int64_t)work.r * c.Hq + work.g * G + head) * D;
+      const bool live = head < G;
+      uint32_t qd[C::INT4 ? 1 : D / 16][2];
+      constexpr int QW = D / (kTwo ? 64 : 32);         // pieces of eight channels
+      f32x2 qf[C::INT4 ? 4 * QW : 1];
+      if constexpr (C::INT4) {
+#pragma unroll
+        for (int i = 0; i < QW; ++i) {
+          const uint4 w = live ? *reinterpret_cast<const uint4*>(q + j * (D / 4) + 8 * (i + (kTwo && n >= 4 ? QW : 0))) : make_uint4(0, 0, 0, 0);
+          qf[4 * i] = pack2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u));
+          qf[4 * i + 1] = pack2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+          qf[4 * i + 2] = pack2(__uint_as_float(w.z << 16), __uint_as_float(w.z & 0xFFFF0000u));
+          qf[4 * i + 3] = pack2(__uint_as_float(w.w << 16), __uint_as_float(w.w & 0xFFFF0000u));
+        }
+      }
+      auto dense_queries = [&](uint32_t (&x)[D / 16][2]) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          x[i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j) : 0u;
+          x[i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * j + 8) : 0u;
+        }
+      };
+      if constexpr (!C::INT4) dense_queries(qd);
+      for (; u0 + warp + k * W < end; ++k) {
+        issue(k + ST - 1);
+        copy_wait<ST - 1>();
+        __syncwarp();
+        const int at = u0 + warp + k * W - work.start;
+        uint8_t* st = my_ring + (size_t)(k % ST) * C::STAGE;
+        if (at < packed) {
+          const int valid = (int)min((int64_t)C::UNIT, work.len.n - (int64_t)at * C::UNIT);
+          if constexpr (C::INT4) int4_unit<D, GROUP, kTwo, PK>(R, qf, smem_addr(st), valid, c.scale2, sp, lane);
+          else dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::K_BYTES, valid, c.scale2, sp, lane);
+        } else {
+          const int valid = min(C::TAIL, work.len.tail - (at - packed) * C::TAIL);
+          if constexpr (C::INT4) {                     // few rows: their queries are read again rather than kept
+            uint32_t x[D / 16][2];
+            dense_queries(x);
+            dense_unit<D, NG, kTwo, 1, PK>(R, x, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
+          } else {
+            dense_unit<D, NG, kTwo, 2, PK>(R, qd, smem_addr(st), smem_addr(st) + C::TAIL * D * 2, valid, c.scale2, sp, lane);
+          }
+        }
+      }
+      open_place();
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) {
+        R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
+        R.sum[1] += __shfl_xor_sync(0xffffffffu, R.sum[1], x);
+      }
+      if (n == 0 && (!kTwo || j < 2)) {
+        m_stat[warp * HEADS + 2 * j] = make_float2(R.ref[0], R.sum[0]);
+        m_stat[warp * HEADS + 2 * j + 1] = make_float2(R.ref[1], R.sum[1]);
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        // channels of the tile's rows lane / 4 and + 8
+        const int ch0 = C::INT4 ? 32 * (i / 2) + 4 * n + 2 * (i & 1) : 16 * i + n, ch1 = C::INT4 ? ch0 + 1 : ch0 + 8;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = R.o[i][e];
+          if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 2);
+          if (!kTwo || j < 2) m_out[(2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
+        }
+      }
+      if constexpr (C::INT4) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          float x, y;
+          unpack2(R.z[i / 2], x, y);
+          if (i & 1) x = y;
+          x += __shfl_xor_sync(0xffffffffu, x, 1);
+          x += __shfl_xor_sync(0xffffffffu, x, 2);
+          if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 16);
+          if (j == 0 && (!kTwo || n < 4)) m_out[HEADS * D + head * NG + i] = x;
+        }
       }
     }
     __syncthreads();
@@ -678,13 +889,13 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
       for (int w = 0; w < W; ++w) {
         const float* of = (const float*)(ring + m_place[w]);
         float x = of[h * D + ch];
-        if constexpr (C::INT4) x += of[HEADS * D + h * NG + ch / GROUP];
+        if constexpr (C::INT4 && !C::F32) x += of[HEADS * D + h * NG + ch / GROUP];
         acc = fmaf(x, m_stat[w * HEADS + h].x, acc);
       }
       const float top = m_total[h].x, sum = m_total[h].y;
       if (whole) {
         const int64_t at = (int64_t)work.r * c.Hq + work.g * G + h;
-        ((__nv_bfloat16*)c.out)[at * D + ch] = __float2bfloat16_rn(acc / sum);
+        narrow((T*)c.out + at * D + ch, acc / sum);
         if (c.lse && ch == 0) c.lse[at] = (top + log2f(sum)) * kLn2;
       } else {
         P.shares[(share * G + h) * D + ch] = acc;
@@ -704,9 +915,9 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
 // Pairs that lie in several CTAs, from the shares these left; and pairs without any row.  A thread sums four channels of
 // every M_PARTS-th share; what it reads first is on its way while the shares' references are compared.
 constexpr int M_THREADS = 512, M_AHEAD = 6;
-template <int D, int GROUP>
+template <typename T, int D, int GROUP>
 __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, int ctas) {
-  using C = RowsCfg<D, GROUP>;
+  using C = RowsCfg<T, D, GROUP>;
   extern __shared__ float m_smem[];                  // [ctas][G] factors; [M_THREADS] partial sums of four channels
   __shared__ float s_top[8], s_sum[8];
   const CacheParams& c = P.c;
@@ -726,7 +937,7 @@ __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, in
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t at = (int64_t)r * c.Hq + g * G;
   if (mine == 0) {
-    for (int i = threadIdx.x; i < G * D; i += M_THREADS) ((__nv_bfloat16*)c.out)[at * D + i] = __float2bfloat16_rn(0.f);
+    for (int i = threadIdx.x; i < G * D; i += M_THREADS) narrow((T*)c.out + at * D + i, 0.f);
     if (c.lse && (int)threadIdx.x < G) c.lse[at + threadIdx.x] = -CUDART_INF_F;
     return;
   }
@@ -782,15 +993,17 @@ __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, in
   if ((int)threadIdx.x >= quads) return;
   for (int y = 1; y < parts; ++y) add(sums[y * quads + quad], 1.f);
   const float inv = 1.f / s_sum[h];
-  reinterpret_cast<uint2*>((__nv_bfloat16*)c.out + at * D)[quad] = make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
+  T* to = (T*)c.out + at * D + 4 * quad;
+  if constexpr (C::F32) *reinterpret_cast<float4*>(to) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+  else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
   if (c.lse && quad % (D / 4) == 0) c.lse[at + h] = (s_top[h] + log2f(s_sum[h])) * kLn2;
 }
 
-template <int D, int GROUP, bool kTwo, int W, int ST>
+template <typename T, int D, int GROUP, bool kTwo, int W, int ST>
 cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
-  using M = RowsSmem<D, GROUP, kTwo, W, ST>;
+  using M = RowsSmem<T, D, GROUP, kTwo, W, ST>;
   static_assert(M::BYTES <= 227 * 1024, "a CTA has 227 KB of shared memory");
-  const auto kernel = attend_units<D, GROUP, kTwo, W, ST>;
+  const auto kernel = attend_units<T, D, GROUP, kTwo, W, ST>;
   static PerDeviceOnce once;
   if (once.need(ctx->device)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::BYTES);
@@ -810,17 +1023,28 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, merge_shares<D, GROUP>, P, ctx->n_sm);
+  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P, ctx->n_sm);
   count_launch(2);
   return e;
 }
 
-template <int D, int GROUP>
+template <typename T, int D, int GROUP>
 cudaError_t run_rows(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
   // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, 4-bit rows 12 x 2 of 2 to
-  // 6 KB (8 warps are as fast, 16 slower by 8 %: they have no more than 128 registers each).
-  constexpr int W = GROUP ? 12 : 4, ST = GROUP ? 2 : 3;
-  return P.c.Hq / P.c.Hkv <= 4 ? run_units<D, GROUP, true, W, ST>(ctx, P, st) : run_units<D, GROUP, false, W, ST>(ctx, P, st);
+  // 6 KB (8 warps are as fast, 16 slower by 8 %: they have no more than 128 registers each); fp32 rows 3 x 2 of up to 32 KB.
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int W = GROUP ? (F32 ? 8 : 12) : F32 ? 3 : 4, ST = GROUP || F32 ? 2 : 3;
+  return P.c.Hq / P.c.Hkv <= 4 ? run_units<T, D, GROUP, true, W, ST>(ctx, P, st) : run_units<T, D, GROUP, false, W, ST>(ctx, P, st);
+}
+template <typename T>
+cudaError_t run_typed(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
+  const bool wide = ctx->cfg.head_dim == 128;
+  switch (P.c.group) {
+    case 0: return wide ? run_rows<T, 128, 0>(ctx, P, st) : run_rows<T, 64, 0>(ctx, P, st);
+    case 32: return wide ? run_rows<T, 128, 32>(ctx, P, st) : run_rows<T, 64, 32>(ctx, P, st);
+    case 64: return wide ? run_rows<T, 128, 64>(ctx, P, st) : run_rows<T, 64, 64>(ctx, P, st);
+    default: return run_rows<T, 128, 128>(ctx, P, st);
+  }
 }
 
 }  // namespace
@@ -835,15 +1059,7 @@ int32_t launch_rows(const cake_ctx* ctx, int32_t n_req, const CacheParams& c, vo
   P.c = c;
   P.shares = (float*)workspace;
   P.n_req = n_req;
-  const bool wide = ctx->cfg.head_dim == 128;
-  cudaError_t e;
-  switch (c.group) {
-    case 0: e = wide ? run_rows<128, 0>(ctx, P, st) : run_rows<64, 0>(ctx, P, st); break;
-    case 32: e = wide ? run_rows<128, 32>(ctx, P, st) : run_rows<64, 32>(ctx, P, st); break;
-    case 64: e = wide ? run_rows<128, 64>(ctx, P, st) : run_rows<64, 64>(ctx, P, st); break;
-    default: e = run_rows<128, 128>(ctx, P, st); break;
-  }
-  return cuda_status(e);
+  return cuda_status(ctx->cfg.dtype == CAKE_DTYPE_FP32 ? run_typed<float>(ctx, P, st) : run_typed<__nv_bfloat16>(ctx, P, st));
 }
 
 }  // namespace cake

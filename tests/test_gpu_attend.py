@@ -6,8 +6,7 @@ the largest over the visible keys; the exponential adds 4 u, relative, and the r
 logits' range, which is at most 2 E.  A weight is therefore off by dw = (2 d + 20) u E + 4 u, relative, and a sum of N of them by
 dw + N u.  An output is a weighted mean: off by (2 dw + 2 N u) S with S = sum_j p_j |v_j|.  bf16: the weights are rounded
 to 2^-8, relative, before they are multiplied with the values (2^-8 S more), and the output is rounded to 2^-8 of itself.
-4-bit keys under bf16 queries: the products q * scale are held in two bf16 terms, 2^-16 relative, and 2^-8 of a weight's product
-with its scale.
+4-bit keys under bf16 queries: the products q * scale are held in two bf16 terms, 2^-16 relative.
 """
 import numpy as np
 import pytest
