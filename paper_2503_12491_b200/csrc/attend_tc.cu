@@ -203,7 +203,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, bool fi
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         const f32x2 x = fma2(pack2(s[64 * half + c + i], s[64 * half + c + i + 1]), sc, mr);
-        if (!kDiag && i == 6) {                  // a quarter of the exponentials on the FMA pipe
+        if (!kDiag && i == 6 && c % 16 == 0) {   // an eighth of the exponentials on the FMA pipe
           exp2_poly(x, e[i], e[i + 1]);
         } else {
           float a, b;
@@ -536,7 +536,7 @@ __device__ __forceinline__ void weigh32(const uint32_t (&r)[32], const float* nl
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const f32x2 x = fma2(pack2(__uint_as_float(r[c + i]), __uint_as_float(r[c + i + 1])), sc, pack2(n[i], n[i + 1]));
-      if (i == 6 || (i == 2 && c % 16 == 0)) {   // three eighths of the exponentials on the FMA pipe
+      if (i == 6) {                              // a quarter of the exponentials on the FMA pipe
         exp2_poly(x, e[i], e[i + 1]);
       } else {
         float a, b;
