@@ -63,6 +63,11 @@ int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const v
                          float* lse, float* lse_window, cudaStream_t st);
 int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
                              cudaStream_t st);
+// attend_tc32.cu
+int32_t launch_prompt_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
+                           float* lse, float* lse_window, cudaStream_t st);
+int32_t launch_accumulate_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
+                               cudaStream_t st);
 // attend_simt.cu
 int32_t launch_prompt_simt(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
                            float* lse, float* lse_window, cudaStream_t st);

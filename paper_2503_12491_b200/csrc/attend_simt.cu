@@ -447,7 +447,7 @@ int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, 
   const bool by_head = out_token_stride >= d && out_head_stride >= d && out_head_stride - d >= (tokens - 1) * out_token_stride;
   if (!by_token && !(heads == 1 && out_token_stride >= d) && !by_head) return CAKE_ERR_ARG;
   const Strided qs = {q_head_stride, q_token_stride}, os = {out_head_stride, out_token_stride};
-  return (prompt_tc_supported(ctx, qs) ? launch_prompt_tc : launch_prompt_simt)(ctx, q, qs, k, v, out, os, lse, lse_window,
+  return (ctx->cfg.dtype == CAKE_DTYPE_FP32 ? launch_prompt_tc32 : launch_prompt_tc)(ctx, q, qs, k, v, out, os, lse, lse_window,
                                                                                 (cudaStream_t)stream);
 }
 
@@ -458,7 +458,7 @@ int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_s
   if (!q || !k || !lse || !out) return CAKE_ERR_ARG;
   if (!rows_ok(ctx, q, q_head_stride, q_token_stride) || !rows_ok(ctx, k, 0, 0)) return CAKE_ERR_ARG;
   const Strided qs = {q_head_stride, q_token_stride};
-  return (prompt_tc_supported(ctx, qs) ? launch_accumulate_tc : launch_accumulate_simt)(ctx, q, qs, k, lse, out, (cudaStream_t)stream);
+  return (ctx->cfg.dtype == CAKE_DTYPE_FP32 ? launch_accumulate_tc32 : launch_accumulate_tc)(ctx, q, qs, k, lse, out, (cudaStream_t)stream);
 }
 
 }  // extern "C"

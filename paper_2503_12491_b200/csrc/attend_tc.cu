@@ -25,19 +25,15 @@
 // tiles on the diagonal: a value that some row of the tile must not see is multiplied by a weight of zero, which only helps
 // if it is finite, so those that are not are zeroed here and added to the rows that do see them at the end.
 // Every wait is bounded; one that runs out raises CAKE_ERR_TIMEOUT and the CTA drains and exits.
-#include "attend.cuh"
-#include "tc_ptx.cuh"
+#include "attend_tc.cuh"
 
 #include <algorithm>
 
 namespace cake {
 namespace {
 
-constexpr int TILE = 128;
-constexpr int SLAB = TILE * 128;                 // bytes of 64 channels of a tile of 128 rows
 constexpr int P_THREADS = 384;
 constexpr int W_TMA = 8, W_MMA = 9, W_SCAN = 10;
-constexpr float kRefSlack = 8.f;                 // powers of two that a row's maximum may lie above its reference
 
 template <int D> struct PromptCfg {
   static constexpr int SLABS = D / 64;
@@ -60,65 +56,6 @@ struct PromptParams {
   int q_head_step, q_token_step;                 // 0 where all heads (tokens) are the same row in memory
   float scale, scale2;
 };
-
-// ------------------------------------------------------------------ PTX
-__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2) {
-  asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
-               "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n}"
-               ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
-// D = A B + (kAcc ? D : 0) with A in tensor memory (16 bf16 of K per step: 8 columns) and B in shared memory, K rows of 64
-// channels in the 128-byte swizzle: the operand's N runs along the row, and beyond 64 channels in the next slab
-// (leading-dimension offset); 8 rows of K are 1024 bytes (stride offset).
-__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\nmov.b64 db, {%2, %5};\n"
-               "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}"
-               ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi) : "memory");
-}
-#define R32(r) "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), \
-  "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), \
-  "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-#define L32 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, " \
-  "%28, %29, %30, %31}"
-// 32 fp32 columns of this thread's TMEM lane (valid after tmem_wait_ld, which must come before any use).
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " L32 ", [%32];" : R32(r) : "r"(addr));
-}
-#define RW32(r) "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), \
-  "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), \
-  "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-// The registers pass through the statement, so that none of their uses is scheduled before it.
-__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) { asm volatile("tcgen05.wait::ld.sync.aligned;" : RW32(r) : : "memory"); }
-__device__ __forceinline__ void pin32(uint32_t* r) { asm volatile("" : RW32(r)); }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-               "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-               "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-               "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
-
-// 2^x of two values on the FMA pipe, x <= 100: x = n + f with n an integer and |f| <= 1/2, 2^f by its minimax polynomial of
-// degree 5 (7.5e-8 relative, a Remez fit), times 2^n put together from its bits: zero from n = -127 down.  A NaN stays one.
-__device__ __forceinline__ f32x2 splat(float x) { return pack2(x, x); }
-__device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
-  float x0, x1;
-  unpack2(x, x0, x1);
-  x = pack2(max_or_nan(x0, -127.f), max_or_nan(x1, -127.f));
-  const f32x2 r = add2(x, splat(12582912.f));                     // 1.5 * 2^23: the integer lands in the low bits
-  const f32x2 f = fma2(add2(r, splat(-12582912.f)), splat(-1.f), x);
-  f32x2 p = fma2(f, splat(1.3276472454890609e-3f), splat(9.675540961325169e-3f));
-  p = fma2(p, f, splat(5.550713092088699e-2f));
-  p = fma2(p, f, splat(2.4022120237350464e-1f));
-  p = fma2(p, f, splat(6.931469440460205e-1f));
-  p = fma2(p, f, splat(1.0000001192092896f));
-  float r0, r1;
-  unpack2(r, r0, r1);
-  unpack2(mul2(p, pack2(__uint_as_float((__float_as_uint(r0) << 23) + 0x3F800000u),
-                        __uint_as_float((__float_as_uint(r1) << 23) + 0x3F800000u))), a, b);
-}
 
 // ------------------------------------------------------------------ prompt
 struct PromptSmem {
@@ -524,37 +461,6 @@ struct AccParams {
   float scale2;
 };
 
-// This thread's key against 32 queries: the sum of its weights.  kEdge: queries before the key, or beyond the prompt, do not
-// count (whatever their logits are).
-template <bool kEdge>
-__device__ __forceinline__ void weigh32(const uint32_t (&r)[32], const float* nl, f32x2 sc, int first, int past, f32x2& acc0, f32x2& acc1) {
-#pragma unroll
-  for (int c = 0; c < 32; c += 8) {
-    float e[8];
-    const float4 n0 = *reinterpret_cast<const float4*>(nl + c), n1 = *reinterpret_cast<const float4*>(nl + c + 4);
-    const float n[8] = {n0.x, n0.y, n0.z, n0.w, n1.x, n1.y, n1.z, n1.w};
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const f32x2 x = fma2(pack2(__uint_as_float(r[c + i]), __uint_as_float(r[c + i + 1])), sc, pack2(n[i], n[i + 1]));
-      if (i == 6) {                              // a quarter of the exponentials on the FMA pipe
-        exp2_poly(x, e[i], e[i + 1]);
-      } else {
-        float a, b;
-        unpack2(x, a, b);
-        e[i] = ex2(a);
-        e[i + 1] = ex2(b);
-      }
-    }
-    if constexpr (kEdge) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = c + i >= first && c + i < past ? e[i] : 0.f;
-    }
-    acc0 = add2(acc0, pack2(e[0], e[1]));
-    acc1 = add2(acc1, pack2(e[2], e[3]));
-    acc0 = add2(acc0, pack2(e[4], e[5]));
-    acc1 = add2(acc1, pack2(e[6], e[7]));
-  }
-}
 template <bool kEdge>
 __device__ __forceinline__ float weigh_tile(uint32_t taddr, const float* nl, float scale2, int first, int past) {
   const f32x2 sc = splat(scale2);
@@ -563,15 +469,15 @@ __device__ __forceinline__ float weigh_tile(uint32_t taddr, const float* nl, flo
   tmem_ld32(taddr, a);
   tmem_wait_ld32(a);
   tmem_ld32(taddr + 32, b);                      // the next columns are on their way during the arithmetic
-  weigh32<kEdge>(a, nl, sc, first, past, acc0, acc1);
+  weigh32<kEdge, true>(a, nl, sc, first, past, acc0, acc1);
   tmem_wait_ld32(b);
   tmem_ld32(taddr + 64, a);
-  weigh32<kEdge>(b, nl + 32, sc, first - 32, past - 32, acc0, acc1);
+  weigh32<kEdge, true>(b, nl + 32, sc, first - 32, past - 32, acc0, acc1);
   tmem_wait_ld32(a);
   tmem_ld32(taddr + 96, b);
-  weigh32<kEdge>(a, nl + 64, sc, first - 64, past - 64, acc0, acc1);
+  weigh32<kEdge, true>(a, nl + 64, sc, first - 64, past - 64, acc0, acc1);
   tmem_wait_ld32(b);
-  weigh32<kEdge>(b, nl + 96, sc, first - 96, past - 96, acc0, acc1);
+  weigh32<kEdge, true>(b, nl + 96, sc, first - 96, past - 96, acc0, acc1);
   float x0, x1, x2, x3;
   unpack2(acc0, x0, x1);
   unpack2(acc1, x2, x3);

@@ -1,0 +1,549 @@
+// Attention over whole prompts in fp32 on the sm_100a tensor cores.
+//
+//   prompt_tc32       O_i = sum_{j<=i} softmax_j(q_i.k_j / sqrt d) v_j and lse_i = log sum_{j<=i} exp(q_i.k_j / sqrt d).
+//   accumulate_tc32   A_j = 1/G sum_h sum_{i>=j} exp(q_hi.k_j / sqrt d - lse_hi).
+//
+// An fp32 number is the exact sum of three bf16 ones (its 24 bits, eight at a time: split8), so a product of two fp32 operands
+// is nine bf16 products, of which the six that reach 2^-24 of the result are taken, the smallest first:
+//     x1 y3 + x3 y1 + x2 y2 + x1 y2 + x2 y1 + x1 y1 ,  summed in fp32 in tensor memory.
+// Six bf16 products are still five times as fast as one in fp32 FMA: 375 against 74 TFLOP/s of the device's nominal rates.
+// (An infinity among what a row sees may make the row a NaN: its second and third terms are NaN.)
+//
+// Operands lie in shared memory as three planes in the 128-byte swizzle; warps of their own read the fp32 rows ahead into
+// registers, split them and write the planes while the tensor cores work on the tile before.  Tiles are 128 rows (keys, for the
+// accumulated attention) by 64: three planes of more do not fit twice.
+// Every wait is bounded; one that runs out raises CAKE_ERR_TIMEOUT and the CTA drains and exits.
+#include "attend_tc.cuh"
+
+#include <algorithm>
+
+namespace cake {
+namespace {
+
+constexpr int STEP = 64;                         // columns of a tile of logits
+constexpr int STEP_SLAB = STEP * 128;            // bytes of 64 channels of a plane of 64 rows
+constexpr int CONV = 128;                        // threads that split one operand
+
+struct Tc32Params {
+  const float *q, *k, *v;
+  float *out, *lse, *lse_window;
+  const float* lse_in;
+  float* acc_out;
+  Strided qs, os;
+  int64_t T;
+  int32_t* status;
+  long long limit;
+  int Hq, Hkv, G, window;
+  float scale2;
+};
+
+// Eight channels: the upper eight bits of every number, the next eight, the rest.
+__device__ __forceinline__ void split8(const float (&x)[8], uint4 (&p)[3]) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = x[2 * i], b = x[2 * i + 1];
+    const float a1 = __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b1 = __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+    const float ra = a - a1, rb = b - b1;
+    const float a2 = __uint_as_float(__float_as_uint(ra) & 0xFFFF0000u), b2 = __uint_as_float(__float_as_uint(rb) & 0xFFFF0000u);
+    w[0][i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    w[1][i] = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
+    w[2][i] = __byte_perm(__float_as_uint(ra - a2), __float_as_uint(rb - b2), 0x7632);
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e) p[e] = make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]);
+}
+// Eight channels of a row, zeros where `in` is false (nothing is read then).
+__device__ __forceinline__ void read8(float (&x)[8], const float* p, bool in) {
+  const float4 a = in ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4 b = in ? __ldg(reinterpret_cast<const float4*>(p) + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+// Planes of piece c (eight channels) of a row, in tiles of ROWS rows.
+template <int D, int ROWS>
+__device__ __forceinline__ void put8(uint8_t* planes, int row, int c, const uint4 (&p)[3]) {
+  uint8_t* at = planes + (c >> 3) * (ROWS * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+#pragma unroll
+  for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(at + e * (ROWS * D * 2)) = p[e];
+}
+__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// A tile of STEP rows, read ahead by CONV threads: 32 to 64 numbers a thread.
+template <int D>
+struct Ahead {
+  static constexpr int PIECES = D / 8, N = STEP * PIECES / CONV;
+  float x[N][8];
+  __device__ __forceinline__ void read(const float* src, int64_t stride, int row0, int valid, int t) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = t + i * CONV, row = row0 + at / PIECES;
+      read8(x[i], src + (int64_t)row * stride + (at % PIECES) * 8, row < valid);
+    }
+  }
+  __device__ __forceinline__ void put(uint8_t* planes, int t) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint4 p[3];
+      split8(x[i], p);
+      put8<D, STEP>(planes, (t + i * CONV) / PIECES, (t + i * CONV) % PIECES, p);
+    }
+  }
+};
+// A tile of 128 rows, once per CTA, by all of its threads.
+template <int D, int THREADS>
+__device__ __forceinline__ void put_tile(uint8_t* planes, const float* src, int64_t stride, int row0, int valid) {
+#pragma unroll 2
+  for (int at = threadIdx.x; at < TILE * (D / 8); at += THREADS) {
+    const int row = at / (D / 8), c = at % (D / 8);
+    float x[8];
+    uint4 p[3];
+    read8(x, src + (int64_t)(row0 + row) * stride + c * 8, row0 + row < valid);
+    split8(x, p);
+    put8<D, TILE>(planes, row, c, p);
+  }
+}
+
+// Planes of the six products.
+__device__ constexpr int first_plane(int e) { return e == 1 ? 2 : e == 2 || e == 4 ? 1 : 0; }
+__device__ constexpr int second_plane(int e) { return e == 0 ? 2 : e == 2 || e == 3 ? 1 : 0; }
+
+// D[128][64] = A B^T over all channels: A planes of 128 rows, B planes of 64 rows, both K-major.
+template <int D>
+__device__ __forceinline__ void products_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+#pragma unroll
+  for (int e = 0; e < 6; ++e) {
+    const uint32_t a = a_lo + first_plane(e) * (uint32_t)(TILE * D * 2 >> 4), b = b_lo + second_plane(e) * (uint32_t)(STEP * D * 2 >> 4);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const uint32_t oa = (ks / 4) * (SLAB >> 4) + (ks % 4) * 2, ob = (ks / 4) * (STEP_SLAB >> 4) + (ks % 4) * 2;
+      if (e == 0 && ks == 0) umma_ss<0>(d, a + oa, b + ob, idesc);
+      else umma_ss<1>(d, a + oa, b + ob, idesc);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ accumulated attention
+constexpr int A_GROUPS = 2, A_CONV = A_GROUPS * 4, A_MMA = A_CONV + 4, A_LSE = A_MMA + 1, A_THREADS = 32 * (A_LSE + 1);
+constexpr int A_BUFS = 4, A_STAGES = 2;
+
+template <int D> constexpr size_t acc32_smem() {
+  return 1024 + (size_t)(TILE + A_STAGES * STEP) * D * 6 + (A_BUFS * STEP + A_GROUPS * TILE) * sizeof(float) + 256;
+}
+
+template <int D>
+__global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_constant__ PromptBatch B, const Tc32Params P) {
+  constexpr int K_BYTES = TILE * D * 6, Q_BYTES = STEP * D * 6;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* qs = ks + K_BYTES;
+  float *nl = (float*)(qs + A_STAGES * Q_BYTES), *part = nl + A_BUFS * STEP;
+  uint64_t *q_full = (uint64_t*)(part + A_GROUPS * TILE), *q_empty = q_full + A_STAGES, *acc_full = q_empty + A_STAGES,
+           *acc_empty = acc_full + A_BUFS, *nl_full = acc_empty + A_BUFS;
+  uint32_t* s_tmem = (uint32_t*)(nl_full + A_BUFS);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int tile = blockIdx.x / P.Hkv, g = blockIdx.x % P.Hkv;
+  const int r = request_of(B, tile), N = B.len[r], key0 = (tile - B.first[r]) * TILE;      // the first keys have the most queries
+  const int64_t cu = B.cu[r];
+  const int per_head = (N - key0 + STEP - 1) / STEP, n_tiles = per_head * P.G;      // query tiles: head by head
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < A_STAGES; ++i) { mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 1); }
+    for (int i = 0; i < A_BUFS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); mbar_init(&nl_full[i], 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == A_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(256) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  put_tile<D, A_THREADS>(ks, P.k + (g * P.T + cu) * D, D, key0, N);
+  async_proxy_fence();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+
+  if (warp == A_MMA) {
+    const uint32_t id = instr_desc(TILE, STEP), a = (smem_u32(ks) & 0x3FFFFu) >> 4, b = (smem_u32(qs) & 0x3FFFFu) >> 4;
+    int last = -1;
+    for (int t = 0; t < n_tiles; ++t) {
+      const int s = t % A_STAGES, buf = t % A_BUFS;
+      if (!mbar_wait(&acc_empty[buf], ((uint32_t)(t / A_BUFS) & 1u) ^ 1u, P.status, P.limit) ||
+          !mbar_wait(&q_full[s], (uint32_t)(t / A_STAGES) & 1u, P.status, P.limit)) break;
+      tc_fence_after();
+      products_ss<D>(tmem + STEP * buf, a, b + (uint32_t)(s * Q_BYTES >> 4), id);
+      umma_commit(&q_empty[s]);
+      umma_commit(&acc_full[buf]);
+      last = t;
+    }
+    // what was issued ends before tensor and shared memory are given back
+    if (last >= 0) mbar_wait(&acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status, P.limit);
+  } else if (warp == A_LSE) {
+    // -lse * log2(e) of the queries of every tile, three tiles ahead in registers
+    constexpr int AHEAD = 3;
+    float x[AHEAD][2];
+    auto get = [&](int t, float (&v)[2]) {
+      const int h = g * P.G + t / per_head, q0 = key0 + (t % per_head) * STEP;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = q0 + 32 * e + lane;
+        v[e] = t < n_tiles && i < N ? -P.lse_in[h * P.T + cu + i] * kLog2E : 0.f;
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) get(u, x[u]);
+    bool ok = true;
+    for (int t0 = 0; t0 < n_tiles && ok; t0 += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int t = t0 + u, buf = t % A_BUFS;
+        if (t >= n_tiles || !ok) break;
+        ok = mbar_wait(&acc_empty[buf], ((uint32_t)(t / A_BUFS) & 1u) ^ 1u, P.status, P.limit);
+        if (!ok) break;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) nl[buf * STEP + 32 * e + lane] = x[u][e];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&nl_full[buf]);
+        get(t + AHEAD, x[u]);
+      }
+    }
+  } else if (warp >= A_CONV) {
+    const int t128 = threadIdx.x - A_CONV * 32;
+    Ahead<D> x;
+    int h = g * P.G, q0 = key0;
+    auto read = [&]() { x.read(P.q + h * P.qs.head + cu * P.qs.token, P.qs.token, q0, N, t128); };
+    read();
+    for (int t = 0; t < n_tiles; ++t) {
+      const int s = t % A_STAGES;
+      if (!mbar_wait(&q_empty[s], ((uint32_t)(t / A_STAGES) & 1u) ^ 1u, P.status, P.limit)) break;
+      x.put(qs + s * Q_BYTES, t128);
+      async_proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[s]);
+      q0 += STEP;
+      if (q0 >= N) { q0 = key0; ++h; }
+      if (t + 1 < n_tiles) read();
+    }
+  } else {
+    const int grp = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const f32x2 sc = splat(P.scale2);
+    float hi = 0.f, lo = 0.f;
+    for (int t = grp; t < n_tiles; t += A_GROUPS) {
+      const int buf = t % A_BUFS, off = (t % per_head) * STEP, past = N - key0 - off;
+      const uint32_t ph = (uint32_t)(t / A_BUFS) & 1u;
+      if (!mbar_wait(&nl_full[buf], ph, P.status, P.limit) || !mbar_wait(&acc_full[buf], ph, P.status, P.limit)) break;
+      tc_fence_after();
+      const uint32_t at = tmem + lanes + STEP * buf;
+      const float* n = nl + buf * STEP;
+      f32x2 acc0 = splat(0.f), acc1 = splat(0.f);
+      uint32_t a[32], b[32];
+      tmem_ld32(at, a);
+      tmem_wait_ld32(a);
+      tmem_ld32(at + 32, b);
+      if (off < TILE || past < STEP) {
+        weigh32<true, false>(a, n, sc, row - off, past, acc0, acc1);
+        tmem_wait_ld32(b);
+        weigh32<true, false>(b, n + 32, sc, row - off - 32, past - 32, acc0, acc1);
+      } else {
+        weigh32<false, false>(a, n, sc, 0, 0, acc0, acc1);
+        tmem_wait_ld32(b);
+        weigh32<false, false>(b, n + 32, sc, 0, 0, acc0, acc1);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      float x0, x1, x2, x3;
+      unpack2(acc0, x0, x1);
+      unpack2(acc1, x2, x3);
+      const float x = (x0 + x1) + (x2 + x3), y = hi + x;
+      lo += hi >= x ? (hi - y) + x : (x - y) + hi;
+      hi = y;
+    }
+    part[grp * TILE + row] = hi + lo;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == A_MMA) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+  } else if (threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
+    P.acc_out[g * P.T + cu + key0 + threadIdx.x] = (part[threadIdx.x] + part[TILE + threadIdx.x]) * (1.f / (float)P.G);
+  }
+}
+
+// ------------------------------------------------------------------ prompt
+// One tile of 128 rows of one query head.  Two buffers of logits: while the softmax of a tile runs, the tensor cores multiply
+// the next tile's, then the weights of this one with its values.
+//   tensor memory: two buffers of 96 columns (64 logits, over which the three planes of weights are written), then O.
+constexpr int P_K = 4, P_V = 8, P_MMA = 12, P_THREADS = 32 * (P_MMA + 1);
+constexpr uint32_t P_BUF = 96, P_OUT = 256;
+
+template <int D> constexpr size_t prompt32_smem() { return 1024 + (size_t)(TILE + 2 * STEP) * D * 6 + 256; }
+
+template <int D>
+__global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constant__ PromptBatch B, const Tc32Params P) {
+  constexpr int Q_BYTES = TILE * D * 6, S_BYTES = STEP * D * 6;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* qs = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t *ks = qs + Q_BYTES, *vs = ks + S_BYTES;
+  uint64_t *k_full = (uint64_t*)(vs + S_BYTES), *k_empty = k_full + 1, *v_full = k_full + 2, *v_empty = k_full + 3, *s_full = k_full + 4,
+           *p_full = k_full + 6, *o_done = k_full + 8;
+  uint32_t* s_tmem = (uint32_t*)(k_full + 9);
+  int* s_dirty = (int*)(k_full + 10);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int tile = blockIdx.x / P.Hq, h = blockIdx.x % P.Hq, g = h / P.G;
+  const int r = request_of(B, tile), N = B.len[r];
+  const int row0 = (B.first[r + 1] - 1 - tile) * TILE;               // the last rows have the most keys: they come first
+  const int64_t cu = B.cu[r];
+  const int n = (min(row0 + TILE, N) + STEP - 1) / STEP;             // key tiles
+
+  if (threadIdx.x == 0) {
+    mbar_init(k_full, 4); mbar_init(k_empty, 1); mbar_init(v_full, 4); mbar_init(v_empty, 1); mbar_init(o_done, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
+    *s_dirty = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == P_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  put_tile<D, P_THREADS>(qs, P.q + h * P.qs.head + cu * P.qs.token, P.qs.token, row0, N);
+  async_proxy_fence();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+
+  if (warp == P_MMA) {
+    const uint32_t id_s = instr_desc(TILE, STEP), id_o = instr_desc(TILE, D) | (1u << 16);     // values: N along the row
+    const uint32_t q_lo = (smem_u32(qs) & 0x3FFFFu) >> 4, k_lo = (smem_u32(ks) & 0x3FFFFu) >> 4;
+    const uint32_t v_lo = ((smem_u32(vs) & 0x3FFFFu) >> 4) | ((uint32_t)(STEP_SLAB >> 4) << 16);
+    bool ok = true;
+    auto qk = [&](int j) {
+      if (!mbar_wait(k_full, (uint32_t)j & 1u, P.status, P.limit)) return false;
+      tc_fence_after();
+      products_ss<D>(tmem + P_BUF * (j & 1), q_lo, k_lo, id_s);
+      umma_commit(k_empty);
+      umma_commit(&s_full[j & 1]);
+      return true;
+    };
+    ok = qk(0);
+    int done = 0;
+    for (int j = 0; ok && j < n; ++j) {
+      // (the next logits take the buffer of the tile before, whose weights the products issued before read)
+      if (j + 1 < n) ok = qk(j + 1);
+      if (ok) ok = mbar_wait(v_full, (uint32_t)j & 1u, P.status, P.limit);
+      if (ok) ok = mbar_wait(&p_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int e = 0; e < 6; ++e) {
+        const uint32_t a = tmem + P_BUF * (j & 1) + 32u * first_plane(e), b = v_lo + second_plane(e) * (uint32_t)(S_BYTES / 3 >> 4);
+#pragma unroll
+        for (int kstep = 0; kstep < STEP / 16; ++kstep)
+          umma_ts(tmem + P_OUT, a + 8 * kstep, b + (uint32_t)(kstep * 2048 >> 4), id_o, (uint32_t)(j > 0 || e > 0 || kstep > 0));
+      }
+      umma_commit(v_empty);
+      umma_commit(o_done);
+      done = j + 1;
+    }
+    if (!ok) {                                   // what was issued ends before tensor and shared memory are given back
+      umma_commit(o_done);
+      mbar_wait(o_done, (uint32_t)done & 1u, P.status, P.limit);
+    }
+  } else if (warp >= P_K) {
+    // K (four warps) and V (four warps): tile by tile
+    const bool is_v = warp >= P_V;
+    const int t128 = threadIdx.x - (is_v ? P_V : P_K) * 32;
+    const float* src = (is_v ? P.v : P.k) + (g * P.T + cu) * D;
+    uint64_t *full = is_v ? v_full : k_full, *empty = is_v ? v_empty : k_empty;
+    uint8_t* planes = is_v ? vs : ks;
+    Ahead<D> x;
+    x.read(src, D, 0, N, t128);
+    for (int j = 0; j < n; ++j) {
+      if (!mbar_wait(empty, ((uint32_t)j & 1u) ^ 1u, P.status, P.limit)) break;
+      if (is_v && (j + 1) * STEP > row0) {
+        // A value that some row of the tile must not see is multiplied by a weight of zero, which only helps if it is finite:
+        // those that are not are added at the end, to the rows that do see them.
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < Ahead<D>::N; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!isfinite(x.x[i][e])) { x.x[i][e] = 0.f; found = true; }
+        if (found) *s_dirty = 1;
+      }
+      x.put(planes, t128);
+      async_proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full);
+      if (j + 1 < n) x.read(src, D, (j + 1) * STEP, N, t128);
+    }
+  } else {
+    const int row = warp * 32 + lane, i = row0 + row;                // in the tile, in the request
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_o = tmem + lanes + P_OUT;
+    float ref = 0.f, sum = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      ok = mbar_wait(&s_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t t_s = tmem + lanes + P_BUF * (j & 1);
+      uint32_t w[64];
+      tmem_ld32(t_s, w);
+      tmem_ld32(t_s + 32, w + 32);
+      tmem_wait_ld32(w);
+      pin32(w + 32);
+      float* s = reinterpret_cast<float*>(w);
+      const int seen = i - j * STEP;             // keys of the tile up to this one are visible
+      if ((j + 1) * STEP > row0 + 1) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) s[c] = c > seen ? -CUDART_INF_F : s[c];
+      }
+      float m0 = s[0], m1 = s[1];
+#pragma unroll
+      for (int c = 2; c < 64; c += 2) { m0 = fmaxf(m0, s[c]); m1 = fmaxf(m1, s[c + 1]); }
+      const float top = fmaxf(m0, m1) * P.scale2;
+      if (j == 0) {
+        ref = top;
+      } else if (__any_sync(0xffffffffu, top > ref + kRefSlack)) {
+        // Some row's maximum left its reference behind: the outputs so far move to the new ones.  (These logits were issued
+        // after the products of tile j - 2, so that at most those of tile j - 1 are still to be waited for.)
+        ok = mbar_wait(o_done, (uint32_t)(j - 1) & 1u, P.status, P.limit);
+        if (!ok) break;
+        tc_fence_after();
+        const float to = top > ref + kRefSlack ? top : ref, f = to == ref ? 1.f : ex2(ref - to);
+        sum *= f;
+        ref = to;
+        uint32_t o[32];
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          tmem_ld32(t_o + c, o);
+          tmem_wait_ld32(o);
+#pragma unroll
+          for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * f);
+          tmem_st32(t_o + c, o);
+        }
+      }
+      // weights, their sum, and their three planes
+      float part[4] = {};
+#pragma unroll
+      for (int c = 0; c < 64; ++c) {
+        s[c] = ex2(fmaf(s[c], P.scale2, -ref));
+        part[c & 3] += s[c];
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        uint32_t p[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          p[c] = __byte_perm(w[2 * c], w[2 * c + 1], 0x7632);
+          if (e < 2) {
+            s[2 * c] -= __uint_as_float(w[2 * c] & 0xFFFF0000u);
+            s[2 * c + 1] -= __uint_as_float(w[2 * c + 1] & 0xFFFF0000u);
+          }
+        }
+        tmem_st32(t_s + 32 * e, p);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[j & 1]);
+    }
+    // (one phase after the other: the products of the tile before the last may not be done either)
+    if (ok && n > 1) ok = mbar_wait(o_done, (uint32_t)n & 1u, P.status, P.limit);
+    if (ok) ok = mbar_wait(o_done, (uint32_t)(n - 1) & 1u, P.status, P.limit);
+    if (ok) {
+      tc_fence_after();
+      const float inv = 1.f / sum;
+      const bool live = i < N;
+      float* dst = P.out + h * P.os.head + (cu + i) * P.os.token;
+      const float* vals = P.v + (g * P.T + cu) * D;
+      const bool dirty = *s_dirty != 0;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        tmem_ld32(t_o + c, o);
+        tmem_wait_ld32(o);
+        float x[32];
+#pragma unroll
+        for (int u = 0; u < 32; ++u) x[u] = __uint_as_float(o[u]) * inv;
+        if (dirty && live) {
+          for (int j = row0 / STEP * STEP; j <= i; ++j)
+#pragma unroll
+            for (int u = 0; u < 32; ++u) {
+              const float y = vals[(int64_t)j * D + c + u];
+              if (!isfinite(y)) x[u] += y;
+            }
+        }
+        if (live) {
+#pragma unroll
+          for (int u = 0; u < 32; u += 4) *reinterpret_cast<float4*>(dst + c + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
+        }
+      }
+      if (live) {
+        const float l = (ref + log2f(sum)) * kLn2;
+        if (P.lse) P.lse[h * P.T + cu + i] = l;
+        const int x = i - (N - P.window);
+        if (P.lse_window && x >= 0) P.lse_window[((int64_t)B.req[r] * P.Hq + h) * P.window + x] = l;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == P_MMA) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host
+Tc32Params common(const cake_ctx* ctx) {
+  const cake_config& c = ctx->cfg;
+  Tc32Params P = {};
+  P.T = ctx->total_tokens; P.status = ctx->d_status;
+  P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
+  P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.G = c.n_q_heads / c.n_kv_heads; P.window = c.window;
+  P.scale2 = kLog2E / sqrtf((float)c.head_dim);
+  return P;
+}
+template <int D, bool kPrompt>
+int32_t run32(const cake_ctx* ctx, const Tc32Params& P, cudaStream_t st) {
+  constexpr size_t smem = kPrompt ? prompt32_smem<D>() : acc32_smem<D>();
+  static_assert(smem <= 227 * 1024, "a CTA has 227 KB of shared memory");
+  const auto kernel = kPrompt ? prompt_tc32<D> : accumulate_tc32<D>;
+  static PerDeviceOnce once;
+  if (once.need(ctx->device)) {
+    CAKE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    once.mark(ctx->device);
+  }
+  PromptBatch B;
+  for (int lo = 0; lo < ctx->n_req; lo += B.n) {
+    fill_prompt_batch(ctx, lo, TILE, B);
+    kernel<<<(unsigned)(B.tiles * (kPrompt ? P.Hq : P.Hkv)), kPrompt ? P_THREADS : A_THREADS, smem, st>>>(B, P);
+    count_launch();
+    CAKE_CUDA_TRY(cudaGetLastError());
+  }
+  return CAKE_OK;
+}
+
+}  // namespace
+
+int32_t launch_prompt_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
+                           float* lse, float* lse_window, cudaStream_t st) {
+  Tc32Params P = common(ctx);
+  P.q = (const float*)q; P.k = (const float*)k; P.v = (const float*)v; P.out = (float*)out; P.lse = lse; P.lse_window = lse_window;
+  P.qs = qs; P.os = os;
+  return ctx->cfg.head_dim == 128 ? run32<128, true>(ctx, P, st) : run32<64, true>(ctx, P, st);
+}
+
+int32_t launch_accumulate_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
+                               cudaStream_t st) {
+  Tc32Params P = common(ctx);
+  P.q = (const float*)q; P.k = (const float*)k; P.lse_in = lse; P.acc_out = out; P.qs = qs;
+  return ctx->cfg.head_dim == 128 ? run32<128, false>(ctx, P, st) : run32<64, false>(ctx, P, st);
+}
+
+}  // namespace cake
