@@ -142,10 +142,11 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
            *acc_empty = acc_full + A_BUFS, *nl_full = acc_empty + A_BUFS;
   uint32_t* s_tmem = (uint32_t*)(nl_full + A_BUFS);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int tile = blockIdx.x / P.Hkv, g = blockIdx.x % P.Hkv;
+  // a cluster of G CTAs, one per query head of the group
+  const int pair = blockIdx.x / P.G, tile = pair / P.Hkv, g = pair % P.Hkv, h = g * P.G + blockIdx.x % P.G;
   const int r = request_of(B, tile), N = B.len[r], key0 = (tile - B.first[r]) * TILE;      // the first keys have the most queries
   const int64_t cu = B.cu[r];
-  const int per_head = (N - key0 + STEP - 1) / STEP, n_tiles = per_head * P.G;      // query tiles: head by head
+  const int n_tiles = (N - key0 + STEP - 1) / STEP;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < A_STAGES; ++i) { mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 1); }
@@ -183,11 +184,10 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
     constexpr int AHEAD = 3;
     float x[AHEAD][2];
     auto get = [&](int t, float (&v)[2]) {
-      const int h = g * P.G + t / per_head, q0 = key0 + (t % per_head) * STEP;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int i = q0 + 32 * e + lane;
-        v[e] = t < n_tiles && i < N ? -P.lse_in[h * P.T + cu + i] * kLog2E : 0.f;
+        const int i = key0 + t * STEP + 32 * e + lane;
+        v[e] = i < N ? -P.lse_in[h * P.T + cu + i] * kLog2E : 0.f;
       }
     };
 #pragma unroll
@@ -210,9 +210,8 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
   } else if (warp >= A_CONV) {
     const int t128 = threadIdx.x - A_CONV * 32;
     Ahead<D> x;
-    int h = g * P.G, q0 = key0;
-    auto read = [&]() { x.read(P.q + h * P.qs.head + cu * P.qs.token, P.qs.token, q0, N, t128); };
-    read();
+    const float* q = P.q + h * P.qs.head + cu * P.qs.token;
+    x.read(q, P.qs.token, key0, N, t128);
     for (int t = 0; t < n_tiles; ++t) {
       const int s = t % A_STAGES;
       if (!mbar_wait(&q_empty[s], ((uint32_t)(t / A_STAGES) & 1u) ^ 1u, P.status, P.limit)) break;
@@ -220,9 +219,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
       async_proxy_fence();
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_full[s]);
-      q0 += STEP;
-      if (q0 >= N) { q0 = key0; ++h; }
-      if (t + 1 < n_tiles) read();
+      if (t + 1 < n_tiles) x.read(q, P.qs.token, key0 + (t + 1) * STEP, N, t128);
     }
   } else {
     const int grp = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -230,7 +227,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
     const f32x2 sc = splat(P.scale2);
     float hi = 0.f, lo = 0.f;
     for (int t = grp; t < n_tiles; t += A_GROUPS) {
-      const int buf = t % A_BUFS, off = (t % per_head) * STEP, past = N - key0 - off;
+      const int buf = t % A_BUFS, off = t * STEP, past = N - key0 - off;
       const uint32_t ph = (uint32_t)(t / A_BUFS) & 1u;
       if (!mbar_wait(&nl_full[buf], ph, P.status, P.limit) || !mbar_wait(&acc_full[buf], ph, P.status, P.limit)) break;
       tc_fence_after();
@@ -267,9 +264,16 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
   if (warp == A_MMA) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
-  } else if (threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
-    P.acc_out[g * P.T + cu + key0 + threadIdx.x] = (part[threadIdx.x] + part[TILE + threadIdx.x]) * (1.f / (float)P.G);
+  } else if (threadIdx.x < TILE) {
+    part[threadIdx.x] += part[TILE + threadIdx.x];
   }
+  cluster_sync();
+  if (cluster_rank() == 0 && threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
+    float x = part[threadIdx.x];
+    for (int y = 1; y < P.G; ++y) x += __uint_as_float(ld_peer(&part[threadIdx.x], (uint32_t)y));
+    P.acc_out[g * P.T + cu + key0 + threadIdx.x] = x * (1.f / (float)P.G);
+  }
+  cluster_sync();                                // nobody leaves while its sums may still be read
 }
 
 // ------------------------------------------------------------------ prompt
@@ -522,9 +526,20 @@ int32_t run32(const cake_ctx* ctx, const Tc32Params& P, cudaStream_t st) {
   PromptBatch B;
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {
     fill_prompt_batch(ctx, lo, TILE, B);
-    kernel<<<(unsigned)(B.tiles * (kPrompt ? P.Hq : P.Hkv)), kPrompt ? P_THREADS : A_THREADS, smem, st>>>(B, P);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(B.tiles * P.Hq), 1, 1);
+    cfg.blockDim = dim3(kPrompt ? P_THREADS : A_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = kPrompt ? 1 : (unsigned)P.G;        // (at most 8: portable)
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    CAKE_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, B, P));
     count_launch();
-    CAKE_CUDA_TRY(cudaGetLastError());
   }
   return CAKE_OK;
 }
