@@ -9,9 +9,11 @@
 // Six bf16 products are still five times as fast as one in fp32 FMA: 375 against 74 TFLOP/s of the device's nominal rates.
 // (An infinity among what a row sees may make the row a NaN: its second and third terms are NaN.)
 //
-// Operands lie in shared memory as three planes in the 128-byte swizzle; warps of their own read the fp32 rows ahead into
-// registers, split them and write the planes while the tensor cores work on the tile before.  Tiles are 128 rows (keys, for the
-// accumulated attention) by 64: three planes of more do not fit twice.
+// The operand that a CTA keeps (128 queries, or keys of the accumulated attention) lies in tensor memory, three planes of d / 2
+// columns, and so do the weights: with both operands in shared memory its bandwidth bounds tiles of this width (6 KB in the
+// 32 cycles of a 128 x 64 x 16 product).  The others come through shared memory in the 128-byte swizzle; warps of their own
+// read the fp32 rows ahead into registers, split them and write the planes while the tensor cores work on the tiles before.
+// Tiles are 64 columns wide: three planes of more do not fit twice.
 // Every wait is bounded; one that runs out raises CAKE_ERR_TIMEOUT and the CTA drains and exits.
 #include "attend_tc.cuh"
 
@@ -90,57 +92,71 @@ struct Ahead {
     }
   }
 };
-// A tile of 128 rows, once per CTA, by all of its threads.
-template <int D, int THREADS>
-__device__ __forceinline__ void put_tile(uint8_t* planes, const float* src, int64_t stride, int row0, int valid) {
-#pragma unroll 2
-  for (int at = threadIdx.x; at < TILE * (D / 8); at += THREADS) {
-    const int row = at / (D / 8), c = at % (D / 8);
-    float x[8];
-    uint4 p[3];
-    read8(x, src + (int64_t)(row0 + row) * stride + c * 8, row0 + row < valid);
-    split8(x, p);
-    put8<D, TILE>(planes, row, c, p);
+// 64 numbers of this thread's lane as three planes of 32 columns, `apart` columns from one another.
+__device__ __forceinline__ void put_planes(uint32_t (&w)[64], uint32_t at, uint32_t apart) {
+#pragma unroll
+  for (int e = 0; e < 3; ++e) {
+    uint32_t p[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      p[c] = __byte_perm(w[2 * c], w[2 * c + 1], 0x7632);
+      if (e < 2) {
+        w[2 * c] = __float_as_uint(__uint_as_float(w[2 * c]) - __uint_as_float(w[2 * c] & 0xFFFF0000u));
+        w[2 * c + 1] = __float_as_uint(__uint_as_float(w[2 * c + 1]) - __uint_as_float(w[2 * c + 1] & 0xFFFF0000u));
+      }
+    }
+    tmem_st32(at + e * apart, p);
   }
+}
+// The row of this thread's lane (zeros if it is not there) as planes of D / 2 columns from `at` on.
+template <int D>
+__device__ __forceinline__ void put_row(const float* src, bool in, uint32_t at) {
+#pragma unroll 1
+  for (int c = 0; c < D; c += 64) {
+    uint32_t w[64];
+#pragma unroll
+    for (int u = 0; u < 64; u += 4) {
+      const float4 x = in ? __ldg(reinterpret_cast<const float4*>(src + c + u)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      w[u] = __float_as_uint(x.x); w[u + 1] = __float_as_uint(x.y); w[u + 2] = __float_as_uint(x.z); w[u + 3] = __float_as_uint(x.w);
+    }
+    put_planes(w, at + c / 2, D / 2);
+  }
+  tmem_wait_st();
 }
 
 // Planes of the six products.
 __device__ constexpr int first_plane(int e) { return e == 1 ? 2 : e == 2 || e == 4 ? 1 : 0; }
 __device__ constexpr int second_plane(int e) { return e == 0 ? 2 : e == 2 || e == 3 ? 1 : 0; }
 
-// D[128][64] = A B^T over all channels: A planes of 128 rows, B planes of 64 rows, both K-major.
+// D[128][64] = A B^T over all channels: A in tensor memory, B planes of 64 rows in shared memory, K-major.
 template <int D>
-__device__ __forceinline__ void products_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+__device__ __forceinline__ void products(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
 #pragma unroll
-  for (int e = 0; e < 6; ++e) {
-    const uint32_t a = a_lo + first_plane(e) * (uint32_t)(TILE * D * 2 >> 4), b = b_lo + second_plane(e) * (uint32_t)(STEP * D * 2 >> 4);
+  for (int e = 0; e < 6; ++e)
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const uint32_t oa = (ks / 4) * (SLAB >> 4) + (ks % 4) * 2, ob = (ks / 4) * (STEP_SLAB >> 4) + (ks % 4) * 2;
-      if (e == 0 && ks == 0) umma_ss<0>(d, a + oa, b + ob, idesc);
-      else umma_ss<1>(d, a + oa, b + ob, idesc);
-    }
-  }
+    for (int ks = 0; ks < D / 16; ++ks)
+      umma_ts(d, a + first_plane(e) * (uint32_t)(D / 2) + 8 * ks,
+              b_lo + second_plane(e) * (uint32_t)(STEP * D * 2 >> 4) + (ks / 4) * (STEP_SLAB >> 4) + (ks % 4) * 2, idesc, (uint32_t)(e > 0 || ks > 0));
 }
 
 // ------------------------------------------------------------------ accumulated attention
 constexpr int A_GROUPS = 2, A_CONV = A_GROUPS * 4, A_MMA = A_CONV + 4, A_LSE = A_MMA + 1, A_THREADS = 32 * (A_LSE + 1);
-constexpr int A_BUFS = 4, A_STAGES = 2;
+constexpr int A_BUFS = 4, A_STAGES = 4;          // tensor memory: four buffers of 64 logits, then the keys
+constexpr uint32_t A_KEYS = A_BUFS * STEP;
 
 template <int D> constexpr size_t acc32_smem() {
-  return 1024 + (size_t)(TILE + A_STAGES * STEP) * D * 6 + (A_BUFS * STEP + A_GROUPS * TILE) * sizeof(float) + 256;
+  return 1024 + (size_t)A_STAGES * STEP * D * 6 + (A_BUFS * STEP + A_GROUPS * TILE) * sizeof(float) + 256;
 }
 
 template <int D>
 __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_constant__ PromptBatch B, const Tc32Params P) {
-  constexpr int K_BYTES = TILE * D * 6, Q_BYTES = STEP * D * 6;
+  constexpr int Q_BYTES = STEP * D * 6;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* qs = ks + K_BYTES;
+  uint8_t* qs = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float *nl = (float*)(qs + A_STAGES * Q_BYTES), *part = nl + A_BUFS * STEP;
   uint64_t *q_full = (uint64_t*)(part + A_GROUPS * TILE), *q_empty = q_full + A_STAGES, *acc_full = q_empty + A_STAGES,
-           *acc_empty = acc_full + A_BUFS, *nl_full = acc_empty + A_BUFS;
-  uint32_t* s_tmem = (uint32_t*)(nl_full + A_BUFS);
+           *acc_empty = acc_full + A_BUFS, *nl_full = acc_empty + A_BUFS, *k_full = nl_full + A_BUFS;
+  uint32_t* s_tmem = (uint32_t*)(k_full + 1);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   // a cluster of G CTAs, one per query head of the group
   const int pair = blockIdx.x / P.G, tile = pair / P.Hkv, g = pair % P.Hkv, h = g * P.G + blockIdx.x % P.G;
@@ -149,30 +165,37 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
   const int n_tiles = (N - key0 + STEP - 1) / STEP;
 
   if (threadIdx.x == 0) {
+    mbar_init(k_full, 4);
     for (int i = 0; i < A_STAGES; ++i) { mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 1); }
     for (int i = 0; i < A_BUFS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); mbar_init(&nl_full[i], 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == A_MMA) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(256) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  put_tile<D, A_THREADS>(ks, P.k + (g * P.T + cu) * D, D, key0, N);
-  async_proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  if (warp < 4) {
+    const int key = key0 + warp * 32 + lane;
+    put_row<D>(P.k + (g * P.T + cu + key) * D, key < N, tmem + ((uint32_t)(warp * 32) << 16) + A_KEYS);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(k_full);
+  }
 
   if (warp == A_MMA) {
-    const uint32_t id = instr_desc(TILE, STEP), a = (smem_u32(ks) & 0x3FFFFu) >> 4, b = (smem_u32(qs) & 0x3FFFFu) >> 4;
+    const uint32_t id = instr_desc(TILE, STEP), b = (smem_u32(qs) & 0x3FFFFu) >> 4;
     int last = -1;
-    for (int t = 0; t < n_tiles; ++t) {
+    const bool ok = mbar_wait(k_full, 0, P.status, P.limit);
+    for (int t = 0; ok && t < n_tiles; ++t) {
       const int s = t % A_STAGES, buf = t % A_BUFS;
       if (!mbar_wait(&acc_empty[buf], ((uint32_t)(t / A_BUFS) & 1u) ^ 1u, P.status, P.limit) ||
           !mbar_wait(&q_full[s], (uint32_t)(t / A_STAGES) & 1u, P.status, P.limit)) break;
       tc_fence_after();
-      products_ss<D>(tmem + STEP * buf, a, b + (uint32_t)(s * Q_BYTES >> 4), id);
+      products<D>(tmem + STEP * buf, tmem + A_KEYS, b + (uint32_t)(s * Q_BYTES >> 4), id);
       umma_commit(&q_empty[s]);
       umma_commit(&acc_full[buf]);
       last = t;
@@ -263,7 +286,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
   __syncthreads();
   if (warp == A_MMA) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   } else if (threadIdx.x < TILE) {
     part[threadIdx.x] += part[TILE + threadIdx.x];
   }
@@ -279,22 +302,22 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
 // ------------------------------------------------------------------ prompt
 // One tile of 128 rows of one query head.  Two buffers of logits: while the softmax of a tile runs, the tensor cores multiply
 // the next tile's, then the weights of this one with its values.
-//   tensor memory: two buffers of 96 columns (64 logits, over which the three planes of weights are written), then O.
+//   tensor memory: two buffers of 96 columns (64 logits, over which the three planes of weights are written), O, the queries.
 constexpr int P_K = 4, P_V = 8, P_MMA = 12, P_THREADS = 32 * (P_MMA + 1);
-constexpr uint32_t P_BUF = 96, P_OUT = 256;
+constexpr uint32_t P_BUF = 96, P_OUT = 192, P_QUERIES = P_OUT + 128;
 
-template <int D> constexpr size_t prompt32_smem() { return 1024 + (size_t)(TILE + 2 * STEP) * D * 6 + 256; }
+template <int D> constexpr size_t prompt32_smem() { return 1024 + (size_t)4 * STEP * D * 6 + 256; }
 
 template <int D>
 __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constant__ PromptBatch B, const Tc32Params P) {
-  constexpr int Q_BYTES = TILE * D * 6, S_BYTES = STEP * D * 6;
+  constexpr int S_BYTES = STEP * D * 6;          // two stages each of K and V
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* qs = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *ks = qs + Q_BYTES, *vs = ks + S_BYTES;
-  uint64_t *k_full = (uint64_t*)(vs + S_BYTES), *k_empty = k_full + 1, *v_full = k_full + 2, *v_empty = k_full + 3, *s_full = k_full + 4,
-           *p_full = k_full + 6, *o_done = k_full + 8;
-  uint32_t* s_tmem = (uint32_t*)(k_full + 9);
-  int* s_dirty = (int*)(k_full + 10);
+  uint8_t* ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* vs = ks + 2 * S_BYTES;
+  uint64_t *k_full = (uint64_t*)(vs + 2 * S_BYTES), *k_empty = k_full + 2, *v_full = k_full + 4, *v_empty = k_full + 6, *s_full = k_full + 8,
+           *p_full = k_full + 10, *o_done = k_full + 12, *q_full = k_full + 13;
+  uint32_t* s_tmem = (uint32_t*)(k_full + 14);
+  int* s_dirty = (int*)(k_full + 15);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int tile = blockIdx.x / P.Hq, h = blockIdx.x % P.Hq, g = h / P.G;
   const int r = request_of(B, tile), N = B.len[r];
@@ -303,8 +326,11 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
   const int n = (min(row0 + TILE, N) + STEP - 1) / STEP;             // key tiles
 
   if (threadIdx.x == 0) {
-    mbar_init(k_full, 4); mbar_init(k_empty, 1); mbar_init(v_full, 4); mbar_init(v_empty, 1); mbar_init(o_done, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
+    mbar_init(o_done, 1); mbar_init(q_full, 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], 1); mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1);
+      mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4);
+    }
     *s_dirty = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -312,8 +338,6 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  put_tile<D, P_THREADS>(qs, P.q + h * P.qs.head + cu * P.qs.token, P.qs.token, row0, N);
-  async_proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -321,34 +345,34 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
 
   if (warp == P_MMA) {
     const uint32_t id_s = instr_desc(TILE, STEP), id_o = instr_desc(TILE, D) | (1u << 16);     // values: N along the row
-    const uint32_t q_lo = (smem_u32(qs) & 0x3FFFFu) >> 4, k_lo = (smem_u32(ks) & 0x3FFFFu) >> 4;
+    const uint32_t k_lo = (smem_u32(ks) & 0x3FFFFu) >> 4;
     const uint32_t v_lo = ((smem_u32(vs) & 0x3FFFFu) >> 4) | ((uint32_t)(STEP_SLAB >> 4) << 16);
-    bool ok = true;
+    bool ok = mbar_wait(q_full, 0, P.status, P.limit);
     auto qk = [&](int j) {
-      if (!mbar_wait(k_full, (uint32_t)j & 1u, P.status, P.limit)) return false;
+      if (!mbar_wait(&k_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit)) return false;
       tc_fence_after();
-      products_ss<D>(tmem + P_BUF * (j & 1), q_lo, k_lo, id_s);
-      umma_commit(k_empty);
+      products<D>(tmem + P_BUF * (j & 1), tmem + P_QUERIES, k_lo + (uint32_t)((j & 1) * S_BYTES >> 4), id_s);
+      umma_commit(&k_empty[j & 1]);
       umma_commit(&s_full[j & 1]);
       return true;
     };
-    ok = qk(0);
+    if (ok) ok = qk(0);
     int done = 0;
     for (int j = 0; ok && j < n; ++j) {
       // (the next logits take the buffer of the tile before, whose weights the products issued before read)
       if (j + 1 < n) ok = qk(j + 1);
-      if (ok) ok = mbar_wait(v_full, (uint32_t)j & 1u, P.status, P.limit);
+      if (ok) ok = mbar_wait(&v_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
       if (ok) ok = mbar_wait(&p_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
       for (int e = 0; e < 6; ++e) {
-        const uint32_t a = tmem + P_BUF * (j & 1) + 32u * first_plane(e), b = v_lo + second_plane(e) * (uint32_t)(S_BYTES / 3 >> 4);
+        const uint32_t a = tmem + P_BUF * (j & 1) + 32u * first_plane(e), b = v_lo + (uint32_t)((j & 1) * S_BYTES >> 4) + second_plane(e) * (uint32_t)(S_BYTES / 3 >> 4);
 #pragma unroll
         for (int kstep = 0; kstep < STEP / 16; ++kstep)
           umma_ts(tmem + P_OUT, a + 8 * kstep, b + (uint32_t)(kstep * 2048 >> 4), id_o, (uint32_t)(j > 0 || e > 0 || kstep > 0));
       }
-      umma_commit(v_empty);
+      umma_commit(&v_empty[j & 1]);
       umma_commit(o_done);
       done = j + 1;
     }
@@ -366,7 +390,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
     Ahead<D> x;
     x.read(src, D, 0, N, t128);
     for (int j = 0; j < n; ++j) {
-      if (!mbar_wait(empty, ((uint32_t)j & 1u) ^ 1u, P.status, P.limit)) break;
+      if (!mbar_wait(&empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u, P.status, P.limit)) break;
       if (is_v && (j + 1) * STEP > row0) {
         // A value that some row of the tile must not see is multiplied by a weight of zero, which only helps if it is finite:
         // those that are not are added at the end, to the rows that do see them.
@@ -378,10 +402,10 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
             if (!isfinite(x.x[i][e])) { x.x[i][e] = 0.f; found = true; }
         if (found) *s_dirty = 1;
       }
-      x.put(planes, t128);
+      x.put(planes + (j & 1) * S_BYTES, t128);
       async_proxy_fence();
       __syncwarp();
-      if (lane == 0) mbar_arrive(full);
+      if (lane == 0) mbar_arrive(&full[j & 1]);
       if (j + 1 < n) x.read(src, D, (j + 1) * STEP, N, t128);
     }
   } else {
@@ -389,6 +413,10 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_o = tmem + lanes + P_OUT;
     float ref = 0.f, sum = 0.f;
     bool ok = true;
+    put_row<D>(P.q + h * P.qs.head + (cu + i) * P.qs.token, i < N, tmem + lanes + P_QUERIES);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(q_full);
     for (int j = 0; j < n; ++j) {
       ok = mbar_wait(&s_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
       if (!ok) break;
@@ -438,19 +466,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
         part[c & 3] += s[c];
       }
       sum += (part[0] + part[1]) + (part[2] + part[3]);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) {
-        uint32_t p[32];
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          p[c] = __byte_perm(w[2 * c], w[2 * c + 1], 0x7632);
-          if (e < 2) {
-            s[2 * c] -= __uint_as_float(w[2 * c] & 0xFFFF0000u);
-            s[2 * c + 1] -= __uint_as_float(w[2 * c + 1] & 0xFFFF0000u);
-          }
-        }
-        tmem_st32(t_s + 32 * e, p);
-      }
+      put_planes(w, t_s, 32);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
