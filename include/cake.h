@@ -334,14 +334,16 @@ int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t
  * query head h reading KV head h / G.
  *   q     H_q * T rows of d elements: row (h, t) at q + h * q_head_stride + t * q_token_stride
  *         ([H_q][T][d]: T*d and d; [T][H_q][d]: d and H_q*d).  Strides in elements, their
- *         bytes multiples of 16, not negative
+ *         bytes multiples of 16; between heads 0 (one set of queries for all) or more, between
+ *         tokens d or more.  H_kv * T < 2^31
  *   k, v  [H_kv][T][d] (packed varlen, as cake_score_layer and cake_compact take them)
  *   out   as q, with strides of its own under which no two rows overlap; must not overlap the inputs
  *   lse   optional [H_q][T] fp32: natural-log sum-exp of each row's scaled logits
  *   lse_window  optional [n_req][H_q][S_w] fp32: the same of the last S_w rows of every request, as
  *         cake_score_layer takes it (its scoring is then one pass instead of two)
  * What lies behind a row (later tokens, other requests) has no influence on it, not even an infinity or
- * a NaN there. */
+ * a NaN there.  (fp32 is computed in three bf16 terms per number, exact to the last bit or two of a finite
+ * one; an infinity that a row does see may make it a NaN.) */
 int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
                            const void* k, const void* v, void* out, int64_t out_head_stride,
                            int64_t out_token_stride, float* lse, float* lse_window, void* stream);

@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "libcake.so")
 PY_SOURCE = os.path.join(CSRC, "py_args.cpp")
 
 SOURCES = ["cake_api.cu", "score_simt.cu", "score_tc.cu", "cascade.cu", "compact.cu",
-           "decode.cu", "quant.cu", "select_static.cu", "attend_simt.cu", "attend_tc.cu", "attend_tc32.cu",
+           "decode.cu", "quant.cu", "select_static.cu", "attend_prompt.cu", "attend_tc.cu", "attend_tc32.cu",
            "attend_cache.cu", "attend_rows.cu"]
 
 

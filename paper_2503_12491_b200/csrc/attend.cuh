@@ -21,7 +21,7 @@ struct PromptBatch {
   int64_t cu[kPromptReqs];             // its first token in the packed batch
 };
 
-// Requests [lo, lo + b.n) of the batch, cut into tiles of `rows` tokens.
+// Requests [lo, lo + b.n) of the batch, cut into tiles of `rows` tokens (attend_prompt.cu).
 void fill_prompt_batch(const cake_ctx* ctx, int lo, int rows, PromptBatch& b);
 
 // The request of a tile (tile < b.tiles).
@@ -58,7 +58,6 @@ struct CacheParams {
 int64_t rows_workspace(const cake_ctx* ctx);
 int32_t launch_rows(const cake_ctx* ctx, int32_t n_req, const CacheParams& c, void* workspace, cudaStream_t st);
 // attend_tc.cu
-bool prompt_tc_supported(const cake_ctx* ctx, Strided q);
 int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
                          float* lse, float* lse_window, cudaStream_t st);
 int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
@@ -67,11 +66,6 @@ int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, con
 int32_t launch_prompt_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
                            float* lse, float* lse_window, cudaStream_t st);
 int32_t launch_accumulate_tc32(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
-                               cudaStream_t st);
-// attend_simt.cu
-int32_t launch_prompt_simt(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
-                           float* lse, float* lse_window, cudaStream_t st);
-int32_t launch_accumulate_simt(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
                                cudaStream_t st);
 
 }  // namespace cake

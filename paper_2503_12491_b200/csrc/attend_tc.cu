@@ -53,7 +53,7 @@ struct PromptParams {
   int32_t* status;
   long long limit;
   int Hq, G, window;
-  int q_head_step, q_token_step;                 // 0 where all heads (tokens) are the same row in memory
+  int q_head_step;                               // 0 where all heads are the same rows in memory
   float scale, scale2;
 };
 
@@ -218,7 +218,7 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
     for (int t = 0; t < (n_b ? 2 : 1); ++t)
       for (int sl = 0; sl < C::SLABS; ++sl)
         tma_load_4d(S.q + t * C::TILE_BYTES + sl * SLAB, &q_map, S.q_full, 64 * sl,
-                    (int)(cu + row0 + t * TILE) * P.q_token_step, h * P.q_head_step, 0);
+                    (int)(cu + row0) + t * TILE, h * P.q_head_step, 0);
     bool ok = true;
     int issued = 0;
     for (int i = 0; i < n_items; ++i) {
@@ -413,13 +413,16 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
 //     D[key][query] = K Q^T  (tcgen05)  ->  sum over the queries of 2^(d * scale - lse)
 // A thread owns a key, so that its sum never leaves its registers; three groups of four warps take the query tiles in turn and
 // are added up at the end in a fixed order.  The queries' log-sum-exps of a tile come through shared memory, where all
-// threads of a warp read the same four at a time.
+// threads of a warp read the same four at a time.  Where there are few tiles of keys, the heads of a group go to CTAs of their
+// own, a cluster, whose first adds up the others' sums (1000 tokens, 32 heads on 8: 26 us before, 14 so; with many tiles the CTAs'
+// beginnings and ends cost more than it gains).
 //
 // Bound.  128 x 128 logits are 512 cycles of the tensor cores and 1024 of the special-function unit: a share of the
 // exponentials is computed on the FMA pipe (exp2_poly), until both units are busy.
 //
 // Sums.  A tile's 128 terms are added in fp32, the tiles' sums with their rounding errors kept (two-part sums).
 constexpr int A_GROUPS = 3, A_THREADS = A_GROUPS * 128 + 128, A_BUFS = 4, A_STAGES = 4;
+constexpr int kFewTiles = 2;                     // tiles of keys per SM below which heads are split
 constexpr int A_TMA = A_GROUPS * 4, A_MMA = A_TMA + 1, A_LSE = A_TMA + 2;
 
 template <int D> constexpr size_t acc_smem() {
@@ -457,7 +460,7 @@ struct AccParams {
   int32_t* status;
   long long limit;
   int Hq, Hkv, G;
-  int q_head_step, q_token_step;
+  int q_head_step;
   float scale2;
 };
 
@@ -484,7 +487,8 @@ __device__ __forceinline__ float weigh_tile(uint32_t taddr, const float* nl, flo
   return (x0 + x1) + (x2 + x3);
 }
 
-template <int D>
+// kSplit: a cluster of G CTAs, one per query head of the group.
+template <int D, bool kSplit>
 __global__ void __launch_bounds__(A_THREADS, 1)
 accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ PromptBatch B,
               const AccParams P) {
@@ -492,10 +496,11 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
   extern __shared__ uint8_t smem_raw[];
   const AccSmem S = carve_acc<D>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int tile = blockIdx.x / P.Hkv, g = blockIdx.x % P.Hkv;
+  const int share = kSplit ? blockIdx.x % P.G : 0, pair = kSplit ? blockIdx.x / P.G : blockIdx.x;
+  const int tile = pair / P.Hkv, g = pair % P.Hkv, h0 = g * P.G + share, heads = kSplit ? 1 : P.G;      // this CTA's query heads
   const int r = request_of(B, tile), N = B.len[r], key0 = (tile - B.first[r]) * TILE;      // the first keys have the most queries
   const int64_t cu = B.cu[r];
-  const int per_head = (N - key0 + TILE - 1) / TILE, n_tiles = per_head * P.G;      // query tiles: head by head
+  const int per_head = (N - key0 + TILE - 1) / TILE, n_tiles = per_head * heads;    // query tiles: head by head
 
   if (threadIdx.x == 0) {
     mbar_init(S.k_full, 1);
@@ -516,7 +521,7 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     mbar_expect_tx(S.k_full, TB);
     tma_load_3d(S.k, &k_map, S.k_full, 0, (int)(g * P.T + cu) + key0, 0);
     bool ok = true;
-    int issued = 0, h = g * P.G, q0 = key0;
+    int issued = 0, h = h0, q0 = key0;
     for (int t = 0; t < n_tiles; ++t) {
       const int s = t % A_STAGES;
       ok = mbar_wait(&S.q_empty[s], ((uint32_t)(t / A_STAGES) & 1u) ^ 1u, P.status, P.limit);
@@ -524,7 +529,7 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
       mbar_expect_tx(&S.q_full[s], TB);
 #pragma unroll
       for (int sl = 0; sl < SLABS; ++sl)
-        tma_load_4d(S.q + s * TB + sl * SLAB, &q_map, &S.q_full[s], 64 * sl, (int)(cu + q0) * P.q_token_step, h * P.q_head_step, 0);
+        tma_load_4d(S.q + s * TB + sl * SLAB, &q_map, &S.q_full[s], 64 * sl, (int)cu + q0, h * P.q_head_step, 0);
       issued = t + 1;
       q0 += TILE;
       if (q0 >= N) { q0 = key0; ++h; }
@@ -567,7 +572,7 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     constexpr int AHEAD = 3;
     float x[AHEAD][4];
     auto get = [&](int t, float (&v)[4]) {
-      const int h = g * P.G + t / per_head, q0 = key0 + (t % per_head) * TILE;
+      const int h = h0 + t / per_head, q0 = key0 + (t % per_head) * TILE;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = q0 + 32 * e + lane;
@@ -617,10 +622,17 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
   if (warp == A_MMA) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
-  } else if (threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
-    P.out[g * P.T + cu + key0 + threadIdx.x] =
-        ((S.part[threadIdx.x] + S.part[128 + threadIdx.x]) + S.part[256 + threadIdx.x]) * (1.f / (float)P.G);
+  } else if (threadIdx.x < TILE) {
+    S.part[threadIdx.x] = (S.part[threadIdx.x] + S.part[128 + threadIdx.x]) + S.part[256 + threadIdx.x];
   }
+  if constexpr (kSplit) cluster_sync();
+  else __syncthreads();
+  if (share == 0 && threadIdx.x < TILE && key0 + (int)threadIdx.x < N) {
+    float x = S.part[threadIdx.x];
+    for (int y = 1; kSplit && y < P.G; ++y) x += __uint_as_float(ld_peer(&S.part[threadIdx.x], (uint32_t)y));
+    P.out[g * P.T + cu + key0 + threadIdx.x] = x * (1.f / (float)P.G);
+  }
+  if constexpr (kSplit) cluster_sync();          // nobody leaves while its sums may still be read
 }
 
 // ------------------------------------------------------------------ host
@@ -637,23 +649,17 @@ bool encode_rows(CUtensorMap* map, const void* p, int64_t rows, int d) {
   const cuuint32_t box[3] = {64, TILE, (cuuint32_t)(d / 64)};
   return encode(map, p, 3, dims, strides, box);
 }
-// Queries as (channels, tokens, heads, 1); an axis whose rows are one row in memory has one entry
+// Queries as (channels, tokens, heads, 1); heads that are the same rows in memory are one
 bool encode_q(CUtensorMap* map, const void* p, const cake_ctx* ctx, Strided s) {
   const cake_config& c = ctx->cfg;
   const cuuint64_t any = 16;
-  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, s.token ? (cuuint64_t)ctx->total_tokens : 1,
-                              s.head ? (cuuint64_t)c.n_q_heads : 1, 1};
-  const cuuint64_t strides[3] = {s.token ? (cuuint64_t)s.token * 2 : any, s.head ? (cuuint64_t)s.head * 2 : any, any};
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)ctx->total_tokens, s.head ? (cuuint64_t)c.n_q_heads : 1, 1};
+  const cuuint64_t strides[3] = {(cuuint64_t)s.token * 2, s.head ? (cuuint64_t)s.head * 2 : any, any};
   const cuuint32_t box[4] = {64, TILE, 1, 1};
   return encode(map, p, 4, dims, strides, box);
 }
 
 }  // namespace
-
-bool prompt_tc_supported(const cake_ctx* ctx, Strided q) {
-  // (all tokens in one row: a box of 128 tokens does not fit such an axis)
-  return ctx->cfg.dtype == CAKE_DTYPE_BF16 && (int64_t)ctx->cfg.n_kv_heads * ctx->total_tokens < ((int64_t)1 << 31) && q.token != 0;
-}
 
 template <int D>
 static cudaError_t run_prompt_tc(const cake_ctx* ctx, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm,
@@ -681,7 +687,7 @@ int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const v
   P.T = ctx->total_tokens; P.status = ctx->d_status;
   P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
   P.Hq = c.n_q_heads; P.G = c.n_q_heads / c.n_kv_heads; P.window = c.window;
-  P.q_head_step = qs.head != 0; P.q_token_step = qs.token != 0;
+  P.q_head_step = qs.head != 0;
   P.scale = 1.f / sqrtf((float)c.head_dim);
   P.scale2 = kLog2E / sqrtf((float)c.head_dim);
   PromptBatch B;
@@ -692,18 +698,30 @@ int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const v
   return CAKE_OK;
 }
 
-template <int D>
+template <int D, bool kSplit>
 static cudaError_t run_accumulate_tc(const cake_ctx* ctx, const CUtensorMap& qm, const CUtensorMap& km, const PromptBatch& B,
                                      const AccParams& P, cudaStream_t st) {
   static PerDeviceOnce once;
   if (once.need(ctx->device)) {
-    const cudaError_t e = cudaFuncSetAttribute(accumulate_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)acc_smem<D>());
+    const cudaError_t e = cudaFuncSetAttribute(accumulate_tc<D, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)acc_smem<D>());
     if (e != cudaSuccess) return e;
     once.mark(ctx->device);
   }
-  accumulate_tc<D><<<(unsigned)(B.tiles * P.Hkv), A_THREADS, acc_smem<D>(), st>>>(qm, km, B, P);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(B.tiles * (kSplit ? P.Hq : P.Hkv)), 1, 1);
+  cfg.blockDim = dim3(A_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = acc_smem<D>();
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)P.G;          // (at most 8: portable)
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = kSplit ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, accumulate_tc<D, kSplit>, qm, km, B, P);
   count_launch();
-  return cudaGetLastError();
+  return e;
 }
 
 int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,
@@ -715,12 +733,14 @@ int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, con
   P.lse = lse; P.out = out; P.T = ctx->total_tokens; P.status = ctx->d_status;
   P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
   P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.G = c.n_q_heads / c.n_kv_heads;
-  P.q_head_step = qs.head != 0; P.q_token_step = qs.token != 0;
+  P.q_head_step = qs.head != 0;
   P.scale2 = kLog2E / sqrtf((float)c.head_dim);
   PromptBatch B;
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {
     fill_prompt_batch(ctx, lo, TILE, B);
-    CAKE_CUDA_TRY(c.head_dim == 128 ? run_accumulate_tc<128>(ctx, qm, km, B, P, st) : run_accumulate_tc<64>(ctx, qm, km, B, P, st));
+    const bool split = P.G > 1 && B.tiles * P.Hkv < kFewTiles * ctx->n_sm;
+    CAKE_CUDA_TRY(c.head_dim == 128 ? (split ? run_accumulate_tc<128, true>(ctx, qm, km, B, P, st) : run_accumulate_tc<128, false>(ctx, qm, km, B, P, st))
+                                    : (split ? run_accumulate_tc<64, true>(ctx, qm, km, B, P, st) : run_accumulate_tc<64, false>(ctx, qm, km, B, P, st)));
   }
   return CAKE_OK;
 }
