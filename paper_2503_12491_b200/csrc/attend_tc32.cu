@@ -24,7 +24,6 @@ namespace {
 
 constexpr int STEP = 64;                         // columns of a tile of logits
 constexpr int STEP_SLAB = STEP * 128;            // bytes of 64 channels of a plane of 64 rows
-constexpr int CONV = 128;                        // threads that split one operand
 
 struct Tc32Params {
   const float *q, *k, *v;
@@ -71,8 +70,8 @@ __device__ __forceinline__ void put8(uint8_t* planes, int row, int c, const uint
 }
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// A tile of STEP rows, read ahead by CONV threads: 32 to 64 numbers a thread.
-template <int D>
+// A tile of STEP rows, read ahead by CONV threads: 16 to 64 numbers a thread.
+template <int D, int CONV>
 struct Ahead {
   static constexpr int PIECES = D / 8, N = STEP * PIECES / CONV;
   float x[N][8];
@@ -232,7 +231,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
     }
   } else if (warp >= A_CONV) {
     const int t128 = threadIdx.x - A_CONV * 32;
-    Ahead<D> x;
+    Ahead<D, 128> x;
     const float* q = P.q + h * P.qs.head + cu * P.qs.token;
     x.read(q, P.qs.token, key0, N, t128);
     for (int t = 0; t < n_tiles; ++t) {
@@ -302,11 +301,16 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
 // ------------------------------------------------------------------ prompt
 // One tile of 128 rows of one query head.  Two buffers of logits: while the softmax of a tile runs, the tensor cores multiply
 // the next tile's, then the weights of this one with its values.
-//   tensor memory: two buffers of 96 columns (64 logits, over which the three planes of weights are written), O, the queries.
-constexpr int P_K = 4, P_V = 8, P_MMA = 12, P_THREADS = 32 * (P_MMA + 1);
+//   tensor memory: two buffers of 96 columns (64 logits, over which the three planes of weights are written), O of one tile, the
+//   queries.
+// Sums in tensor memory are truncated, not rounded: half a step off per addition on average, and always downwards.  Over the
+// tiles of a prompt that adds up (2.2e-6 relative at 512 keys), so the products of a tile of keys are added to the outputs so far
+// in registers: a thread of the eight warps that split K and V has half of a row's channels.
+//   Warps: 0-3 softmax, 4-11 K and V into planes and the outputs, 12 MMAs and tensor-memory allocation.
+constexpr int P_CONV = 4, P_MMA = 12, P_THREADS = 32 * (P_MMA + 1), P_FACTORS = 4;
 constexpr uint32_t P_BUF = 96, P_OUT = 192, P_QUERIES = P_OUT + 128;
 
-template <int D> constexpr size_t prompt32_smem() { return 1024 + (size_t)4 * STEP * D * 6 + 256; }
+template <int D> constexpr size_t prompt32_smem() { return 1024 + (size_t)4 * STEP * D * 6 + (P_FACTORS + 1) * TILE * sizeof(float) + 256; }
 
 template <int D>
 __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constant__ PromptBatch B, const Tc32Params P) {
@@ -314,24 +318,29 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* vs = ks + 2 * S_BYTES;
-  uint64_t *k_full = (uint64_t*)(vs + 2 * S_BYTES), *k_empty = k_full + 2, *v_full = k_full + 4, *v_empty = k_full + 6, *s_full = k_full + 8,
-           *p_full = k_full + 10, *o_done = k_full + 12, *q_full = k_full + 13;
-  uint32_t* s_tmem = (uint32_t*)(k_full + 14);
-  int* s_dirty = (int*)(k_full + 15);
+  float* factors = (float*)(vs + 2 * S_BYTES);   // [P_FACTORS][128] what a row's outputs so far are multiplied with at a tile
+  float* sums = factors + P_FACTORS * TILE;      // [128]
+  uint64_t *k_full = (uint64_t*)(sums + TILE), *k_empty = k_full + 2, *v_full = k_full + 4, *v_empty = k_full + 6, *s_full = k_full + 8,
+           *p_full = k_full + 10, *o_full = k_full + 12, *o_empty = k_full + 13, *q_full = k_full + 14;
+  uint32_t* s_tmem = (uint32_t*)(k_full + 15);
+  int* s_dirty = (int*)(k_full + 16);
+  int* s_failed = s_dirty + 1;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int tile = blockIdx.x / P.Hq, h = blockIdx.x % P.Hq, g = h / P.G;
   const int r = request_of(B, tile), N = B.len[r];
   const int row0 = (B.first[r + 1] - 1 - tile) * TILE;               // the last rows have the most keys: they come first
   const int64_t cu = B.cu[r];
   const int n = (min(row0 + TILE, N) + STEP - 1) / STEP;             // key tiles
+  const int row = (warp & 3) * 32 + lane, i = row0 + row;            // of a softmax or output thread: in the tile, in the request
+  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
 
   if (threadIdx.x == 0) {
-    mbar_init(o_done, 1); mbar_init(q_full, 4);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], 1); mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1);
-      mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4);
+    mbar_init(o_full, 1); mbar_init(o_empty, 8); mbar_init(q_full, 4);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&k_full[x], 8); mbar_init(&k_empty[x], 1); mbar_init(&v_full[x], 8); mbar_init(&v_empty[x], 1);
+      mbar_init(&s_full[x], 1); mbar_init(&p_full[x], 4);
     }
-    *s_dirty = 0;
+    *s_dirty = *s_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == P_MMA) {
@@ -342,6 +351,10 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  constexpr int DH = D / 2;                      // channels of an output thread
+  float o[DH];                                   // (warps 4 to 11)
+#pragma unroll
+  for (int c = 0; c < DH; ++c) o[c] = 0.f;
 
   if (warp == P_MMA) {
     const uint32_t id_s = instr_desc(TILE, STEP), id_o = instr_desc(TILE, D) | (1u << 16);     // values: N along the row
@@ -363,54 +376,81 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
       if (j + 1 < n) ok = qk(j + 1);
       if (ok) ok = mbar_wait(&v_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
       if (ok) ok = mbar_wait(&p_full[j & 1], (uint32_t)(j >> 1) & 1u, P.status, P.limit);
+      if (ok) ok = mbar_wait(o_empty, ((uint32_t)j & 1u) ^ 1u, P.status, P.limit);
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
       for (int e = 0; e < 6; ++e) {
-        const uint32_t a = tmem + P_BUF * (j & 1) + 32u * first_plane(e), b = v_lo + (uint32_t)((j & 1) * S_BYTES >> 4) + second_plane(e) * (uint32_t)(S_BYTES / 3 >> 4);
+        const uint32_t a = tmem + P_BUF * (j & 1) + 32u * first_plane(e);
+        const uint32_t b = v_lo + (uint32_t)((j & 1) * S_BYTES >> 4) + second_plane(e) * (uint32_t)(S_BYTES / 3 >> 4);
 #pragma unroll
         for (int kstep = 0; kstep < STEP / 16; ++kstep)
-          umma_ts(tmem + P_OUT, a + 8 * kstep, b + (uint32_t)(kstep * 2048 >> 4), id_o, (uint32_t)(j > 0 || e > 0 || kstep > 0));
+          umma_ts(tmem + P_OUT, a + 8 * kstep, b + (uint32_t)(kstep * 2048 >> 4), id_o, (uint32_t)(e > 0 || kstep > 0));
       }
       umma_commit(&v_empty[j & 1]);
-      umma_commit(o_done);
+      umma_commit(o_full);
       done = j + 1;
     }
     if (!ok) {                                   // what was issued ends before tensor and shared memory are given back
-      umma_commit(o_done);
-      mbar_wait(o_done, (uint32_t)done & 1u, P.status, P.limit);
+      umma_commit(o_full);
+      mbar_wait(o_full, (uint32_t)done & 1u, P.status, P.limit);
     }
-  } else if (warp >= P_K) {
-    // K (four warps) and V (four warps): tile by tile
-    const bool is_v = warp >= P_V;
-    const int t128 = threadIdx.x - (is_v ? P_V : P_K) * 32;
-    const float* src = (is_v ? P.v : P.k) + (g * P.T + cu) * D;
-    uint64_t *full = is_v ? v_full : k_full, *empty = is_v ? v_empty : k_empty;
-    uint8_t* planes = is_v ? vs : ks;
-    Ahead<D> x;
-    x.read(src, D, 0, N, t128);
-    for (int j = 0; j < n; ++j) {
-      if (!mbar_wait(&empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u, P.status, P.limit)) break;
-      if (is_v && (j + 1) * STEP > row0) {
+  } else if (warp >= P_CONV) {
+    const int t256 = threadIdx.x - P_CONV * 32, c0 = ((warp - P_CONV) >> 2) * DH;
+    const float *k = P.k + (g * P.T + cu) * D, *v = P.v + (g * P.T + cu) * D;
+    Ahead<D, 256> x;                             // the next tile: K of 0, then K of j + 1 and V of j in turn
+    auto put = [&](uint8_t* planes, uint64_t* full, uint64_t* empty, int j) {
+      if (!mbar_wait(&empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u, P.status, P.limit)) return false;
+      x.put(planes + (j & 1) * S_BYTES, t256);
+      async_proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[j & 1]);
+      return true;
+    };
+    // tile j's products to the outputs, which move to its reference
+    auto add = [&](int j) {
+      if (!mbar_wait(o_full, (uint32_t)j & 1u, P.status, P.limit)) return false;
+      tc_fence_after();
+      const float f = factors[(j % P_FACTORS) * TILE + row];
+#pragma unroll
+      for (int c = 0; c < DH; c += 16) {
+        uint32_t w[16];
+        tmem_ld16_issue(tmem + lanes + P_OUT + c0 + c, w);
+        tmem_ld_wait(w);
+#pragma unroll
+        for (int u = 0; u < 16; ++u) o[c + u] = fmaf(o[c + u], f, __uint_as_float(w[u]));
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(o_empty);
+      return true;
+    };
+    x.read(k, D, 0, N, t256);
+    bool ok = put(ks, k_full, k_empty, 0);
+    if (n > 1) x.read(k, D, STEP, N, t256);
+    for (int j = 0; j < n && ok; ++j) {
+      if (j + 1 < n) ok = put(ks, k_full, k_empty, j + 1);
+      if (!ok) break;
+      x.read(v, D, j * STEP, N, t256);
+      if (j > 0) ok = add(j - 1);                // (the values are on their way)
+      if (!ok) break;
+      if ((j + 1) * STEP > row0) {
         // A value that some row of the tile must not see is multiplied by a weight of zero, which only helps if it is finite:
         // those that are not are added at the end, to the rows that do see them.
         bool found = false;
 #pragma unroll
-        for (int i = 0; i < Ahead<D>::N; ++i)
+        for (int y = 0; y < Ahead<D, 256>::N; ++y)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (!isfinite(x.x[i][e])) { x.x[i][e] = 0.f; found = true; }
+            if (!isfinite(x.x[y][e])) { x.x[y][e] = 0.f; found = true; }
         if (found) *s_dirty = 1;
       }
-      x.put(planes + (j & 1) * S_BYTES, t128);
-      async_proxy_fence();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&full[j & 1]);
-      if (j + 1 < n) x.read(src, D, (j + 1) * STEP, N, t128);
+      ok = put(vs, v_full, v_empty, j);
+      if (j + 2 < n) x.read(k, D, (j + 2) * STEP, N, t256);
     }
+    if (ok) ok = add(n - 1);
+    if (!ok) *s_failed = 1;
   } else {
-    const int row = warp * 32 + lane, i = row0 + row;                // in the tile, in the request
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16, t_o = tmem + lanes + P_OUT;
     float ref = 0.f, sum = 0.f;
     bool ok = true;
     put_row<D>(P.q + h * P.qs.head + (cu + i) * P.qs.token, i < N, tmem + lanes + P_QUERIES);
@@ -437,27 +477,11 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
 #pragma unroll
       for (int c = 2; c < 64; c += 2) { m0 = fmaxf(m0, s[c]); m1 = fmaxf(m1, s[c + 1]); }
       const float top = fmaxf(m0, m1) * P.scale2;
-      if (j == 0) {
-        ref = top;
-      } else if (__any_sync(0xffffffffu, top > ref + kRefSlack)) {
-        // Some row's maximum left its reference behind: the outputs so far move to the new ones.  (These logits were issued
-        // after the products of tile j - 2, so that at most those of tile j - 1 are still to be waited for.)
-        ok = mbar_wait(o_done, (uint32_t)(j - 1) & 1u, P.status, P.limit);
-        if (!ok) break;
-        tc_fence_after();
-        const float to = top > ref + kRefSlack ? top : ref, f = to == ref ? 1.f : ex2(ref - to);
-        sum *= f;
-        ref = to;
-        uint32_t o[32];
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          tmem_ld32(t_o + c, o);
-          tmem_wait_ld32(o);
-#pragma unroll
-          for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * f);
-          tmem_st32(t_o + c, o);
-        }
-      }
+      // The reference follows a maximum that is more than 2^kRefSlack above it.  (A factor is read before the logits of three
+      // tiles on are issued, so that a ring of four is enough.)
+      const float to = j == 0 || top > ref + kRefSlack ? top : ref, f = j == 0 || to == ref ? 1.f : ex2(ref - to);
+      ref = to;
+      factors[(j % P_FACTORS) * TILE + row] = f;
       // weights, their sum, and their three planes
       float part[4] = {};
 #pragma unroll
@@ -465,50 +489,20 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
         s[c] = ex2(fmaf(s[c], P.scale2, -ref));
         part[c & 3] += s[c];
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      sum = fmaf(sum, f, (part[0] + part[1]) + (part[2] + part[3]));
       put_planes(w, t_s, 32);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_full[j & 1]);
     }
-    // (one phase after the other: the products of the tile before the last may not be done either)
-    if (ok && n > 1) ok = mbar_wait(o_done, (uint32_t)n & 1u, P.status, P.limit);
-    if (ok) ok = mbar_wait(o_done, (uint32_t)(n - 1) & 1u, P.status, P.limit);
-    if (ok) {
-      tc_fence_after();
-      const float inv = 1.f / sum;
-      const bool live = i < N;
-      float* dst = P.out + h * P.os.head + (cu + i) * P.os.token;
-      const float* vals = P.v + (g * P.T + cu) * D;
-      const bool dirty = *s_dirty != 0;
-#pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        tmem_ld32(t_o + c, o);
-        tmem_wait_ld32(o);
-        float x[32];
-#pragma unroll
-        for (int u = 0; u < 32; ++u) x[u] = __uint_as_float(o[u]) * inv;
-        if (dirty && live) {
-          for (int j = row0 / STEP * STEP; j <= i; ++j)
-#pragma unroll
-            for (int u = 0; u < 32; ++u) {
-              const float y = vals[(int64_t)j * D + c + u];
-              if (!isfinite(y)) x[u] += y;
-            }
-        }
-        if (live) {
-#pragma unroll
-          for (int u = 0; u < 32; u += 4) *reinterpret_cast<float4*>(dst + c + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
-        }
-      }
-      if (live) {
-        const float l = (ref + log2f(sum)) * kLn2;
-        if (P.lse) P.lse[h * P.T + cu + i] = l;
-        const int x = i - (N - P.window);
-        if (P.lse_window && x >= 0) P.lse_window[((int64_t)B.req[r] * P.Hq + h) * P.window + x] = l;
-      }
+    if (!ok) *s_failed = 1;
+    sums[row] = sum;
+    if (ok && i < N) {
+      const float l = (ref + log2f(sum)) * kLn2;
+      if (P.lse) P.lse[h * P.T + cu + i] = l;
+      const int x = i - (N - P.window);
+      if (P.lse_window && x >= 0) P.lse_window[((int64_t)B.req[r] * P.Hq + h) * P.window + x] = l;
     }
   }
   tc_fence_before();
@@ -516,6 +510,23 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
   if (warp == P_MMA) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  } else if (warp >= P_CONV && i < N && !*s_failed) {
+    const int c0 = ((warp - P_CONV) >> 2) * DH;
+    const float inv = 1.f / sums[row];
+    float* dst = P.out + h * P.os.head + (cu + i) * P.os.token + c0;
+#pragma unroll
+    for (int c = 0; c < DH; ++c) o[c] *= inv;
+    if (*s_dirty) {
+      const float* vals = P.v + (g * P.T + cu) * D + c0;
+      for (int j = row0; j <= i; ++j)
+#pragma unroll
+        for (int c = 0; c < DH; ++c) {
+          const float y = vals[(int64_t)j * D + c];
+          if (!isfinite(y)) o[c] += y;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < DH; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
   }
 }
 
