@@ -534,3 +534,82 @@ def test_attention_output_of_a_decode_step():
                     want = O.attend(f64(q)[r, h * 4:h * 4 + 4], f64(kc[rows]), f64(vc[rows]))
                     dw = weight_error(f64(q)[r, h * 4:h * 4 + 4], f64(kc[rows]), d)
                     check_out(f64(out)[r, h * 4:h * 4 + 4], f64(lse)[r, h * 4:h * 4 + 4], want, dw, n, BF16)
+
+
+# ------------------------------------------------------------------ large
+@pytest.mark.parametrize("dtype,n", [(BF16, 20011), (FP32, 9001)], ids=["bf16", "fp32"])
+def test_long_prompt_rows(dtype, n):
+    """Rows of a long prompt, at the tiles' borders and between, and the columns' sums from the device's own rows."""
+    cake = context(4, 2, 128, dtype, (n,))
+    q, k, v = prompt(4, 2, 128, dtype, (n,))
+    out, lse = cake.attend_prompt(q, k, v)
+    kn, vn = f64(k), f64(v)
+    rows = [0, 127, 128, 255, 256, 8191, 8192, n - 130, n - 2, n - 1] + list(np.random.default_rng(1).integers(0, n, 20))
+    for h in range(4):
+        for i in rows:
+            want = O.attend(f64(q[h, i:i + 1]), kn[h // 2, :i + 1], vn[h // 2, :i + 1])
+            dw = weight_error(f64(q[h, i:i + 1]), kn[h // 2, :i + 1], 128)
+            check_out(f64(out[h, i:i + 1]), f64(lse[h, i:i + 1]), want, dw, i + 1, dtype)
+    got = f64(cake.accumulate_attention(q, k, lse))
+    ln, qn = f64(lse), f64(q)
+    for j in (0, 5, 127, 128, 4099, n - 64, n - 1):
+        for g in range(2):
+            s = (qn[2 * g:2 * g + 2, j:] @ kn[g, j]) / np.sqrt(128.0)
+            ref = np.exp(s - ln[2 * g:2 * g + 2, j:]).sum() / 2
+            dw = weight_error(qn[2 * g:2 * g + 2], kn[g, j:j + 1], 128)
+            assert abs(got[g, j] - ref) <= (2 * dw + 4 * U * np.abs(ln).max() + 2 * n * U) * ref
+
+
+@pytest.mark.parametrize("group", [0, 32])
+def test_cache_offsets_beyond_32_bits(group):
+    """The block lies beyond 2^31 elements (bytes of codes) of its buffers."""
+    d, n, first = 128, 700, 17_000_000 if group == 0 else 34_000_000
+    rows = first + 2 * n
+    cake = context(8, 2, d, BF16, layers=2)
+    x = cached(8, 2, d, BF16, (n,), group, layers=1, layer=0)
+    x["layer"] = 1
+    far = torch.tensor([0, first, rows], dtype=torch.int64, device="cuda")
+    if group == 0:
+        big = {m: torch.empty(rows, d, dtype=BF16, device="cuda") for m in "kv"}
+        for m in "kv":
+            big[m][first:] = x[m][:2 * n]
+        got = cake.attend_cache(1, x["q"], big["k"], big["v"], far)
+        want = context(8, 2, d, BF16).attend_cache(0, x["q"], x["k"], x["v"], x["off"])
+    else:
+        c = x["cache"]
+        groups = 2 * -(-n // group)
+        big = {m: torch.empty(rows, *t.shape[1:], dtype=t.dtype, device="cuda") for m, t in c.items() if m in ("k_codes", "v_codes", "v_scale", "v_zero")}
+        for m in big:
+            big[m][first:] = c[m][:2 * n]
+        start = first // group
+        for m in ("k_scale", "k_zero"):
+            big[m] = torch.empty(start + groups, d, device="cuda")
+            big[m][start:] = c[m][:groups]
+        big.update(row_offsets=far, kgroup_offsets=torch.tensor([0, start, start + groups], dtype=torch.int64, device="cuda"))
+        got = cake.attend_int4(1, x["q"], big)
+        want = context(8, 2, d, BF16).attend_int4(0, x["q"], c)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+def test_prompt_offsets_beyond_32_bits(layout):
+    """The last requests of a batch whose queries and outputs have more than 2^31 elements."""
+    hq, hkv, d, many, each = 16, 2, 128, 1200, 900
+    lens = (each,) * many
+    T = sum(lens)
+    cake = context(hq, hkv, d, BF16, lens)
+    q = torch.zeros((hq, T, d) if layout == "heads" else (T, hq, d), dtype=BF16, device="cuda")
+    q = q if layout == "heads" else q.transpose(0, 1)
+    k, v = torch.zeros(hkv, T, d, dtype=BF16, device="cuda"), torch.zeros(hkv, T, d, dtype=BF16, device="cuda")
+    qs, ks, vs = prompt(hq, hkv, d, BF16, (each, each))
+    q[:, T - 2 * each:], k[:, T - 2 * each:], v[:, T - 2 * each:] = qs, ks, vs
+    out, lse = cake.attend_prompt(q, k, v)
+    got = cake.accumulate_attention(q, k, lse)
+    small = context(hq, hkv, d, BF16, (each, each))
+    want, want_lse = small.attend_prompt(qs, ks, vs)
+    assert q.numel() > 2 ** 31
+    assert torch.equal(out[:, T - 2 * each:], want) and torch.equal(lse[:, T - 2 * each:], want_lse)
+    one = got[:, T - 2 * each:]
+    ref = small.accumulate_attention(qs, ks, want_lse)
+    assert (one - ref).abs().max() <= 1e-5 * ref.abs().max()       # (few keys: their heads are split over CTAs)
+    cake.destroy()
