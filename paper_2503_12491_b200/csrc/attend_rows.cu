@@ -2,12 +2,6 @@
 // either the rows of tokens generated since.
 //
 //   O_h = sum_j softmax_j(q_h.k_j / sqrt d) v_j ,  lse_h = log sum_j exp(q_h.k_j / sqrt d)   over all rows j of h's KV head.
-#include "cache_mma.cuh"
-#include "tc_ptx.cuh"
-
-namespace cake {
-namespace {
-
 //
 // Work.  The (request, KV head) pairs of the layer are cut into units of 32 rows (the tail's rows behind the packed ones; 8 rows
 // a unit in the 4-bit kernel, whose stages are smaller), and every CTA of one per SM takes the same number of consecutive
@@ -15,12 +9,14 @@ namespace {
 // the device, so each CTA adds up the units of all requests for itself.  Inside a CTA the warps take the units in turn, each
 // with copies of its own units in flight (cp.async) and its own running softmax; they meet only where a pair ends.  A pair that
 // lies in one CTA is finished there; of the others a CTA leaves its share in the workspace (at most one share at either end
-// of its run), and merge_shares, which waits for the last CTA on its SMs, puts them together.
+// of its run), and merge_shares, a CTA per boundary between two runs, puts them together: no CTA waits for another, and the
+// workspace needs no initialisation.  (In one launch instead: by clusters of 16 CTAs per head 11.2 us for one request of 2048 rows
+// and 8 heads, where this takes 8.0; by the CTA that leaves a pair's last share, counted with atomics, 16.4.)
 //
-// bf16 queries: products on the tensor cores (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the query heads as the 8 columns.  With
-// up to four heads the columns 4 to 7 hold the same heads once more, for the second term of what is held in two bf16 terms
-// (kTwo): weights, and queries and weights times scales, are then exact to 2^-16.  With more heads the 4-bit kernel
-// multiplies twice, and the weights of bf16 rows are rounded to bf16.
+// bf16 queries: products on the tensor cores (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the
+// query heads as the 8 columns.  With up to four heads the columns 4 to 7 hold the same heads once more, for the second term of
+// what is held in two bf16 terms (kTwo): weights, and queries and weights times scales, are then exact to 2^-16.  With more heads
+// the 4-bit kernel multiplies twice, and the weights of bf16 rows are rounded to bf16.
 //
 // 4-bit rows.  A code c becomes the bf16 16 + c (or 128 + c) by a logical operation per pair and at most one shift; scales and
 // zeros are never applied to a row but to the other operand: q_c s_c for the keys, p_j s_j for the values, and
@@ -29,6 +25,16 @@ namespace {
 // products of that rounded operand with a constant (the tensor cores are idle for the most part; logical operations set the
 // pace).  Channels and keys are taken in whatever order the words bring them, the same one in both operands; a value tile's 16
 // channels come from one group of 32, which has one scale per row.
+//
+// Bound.  bf16 and fp32 rows: DRAM, 5.9 TB/s of the 6.5 that a copy reaches (32 requests of 1000 to 6000 rows, 8 heads).  4-bit
+// rows: a unit of 32 rows and 128 channels is about 1050 instructions of a warp, half of them logical operations or additions of
+// whole numbers at two cycles each, and 72 products at eight: 2.5 TB/s (84 us for 32 requests of 1000 to 8000 rows; 32 us of DRAM).
+#include "cache_mma.cuh"
+#include "tc_ptx.cuh"
+
+namespace cake {
+namespace {
+
 constexpr float kRefSlack = 8.f;                 // powers of two a maximum may lie above the reference before all is rescaled
 
 template <typename T, int D, int GROUP> struct RowsCfg {
@@ -90,14 +96,15 @@ struct Requests {
     }
     upto = lanes_before(units, lane);
   }
-  __device__ __forceinline__ void read_all(const CacheParams& c, int n_req, int lane) {
+  // All of them, the first ones last (they stay); each(base) after every 32.
+  template <typename F>
+  __device__ __forceinline__ void read_all(const CacheParams& c, int n_req, int lane, F each) {
     all = 0;
-    for (int base = 32; base < n_req; base += 32) {
+    for (int base = (n_req - 1) / 32 * 32; base >= 0; base -= 32) {
       read(c, n_req, base, lane);
       all += __shfl_sync(0xffffffffu, upto, 31);
+      each(base);
     }
-    read(c, n_req, 0, lane);
-    all += __shfl_sync(0xffffffffu, upto, 31);
   }
 };
 // (Units are counted in 32 bits: 2^31 of them are 4 TB of 4-bit rows.)
@@ -677,7 +684,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
 
   // --- this CTA's units, and the pair of the first
   Requests<C::UNIT, C::TAIL> Q;
-  Q.read_all(c, P.n_req, lane);
+  Q.read_all(c, P.n_req, lane, [](int) {});
   const int total = Q.all * c.Hkv, per = per_cta(total, gridDim.x);
   const int u0 = (int)min((int64_t)total, (int64_t)blockIdx.x * per), u1 = min(u0 + per, total);
   if (u0 >= u1) return;
@@ -912,37 +919,36 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   copy_wait<0>();
 }
 
-// Pairs that lie in several CTAs, from the shares these left; and pairs without any row.  A thread sums four channels of
-// every M_PARTS-th share; what it reads first is on its way while the shares' references are compared.
+// Pairs that lie in several CTAs, from the shares these left: the pair that goes on from CTA blockIdx.x to the next, if it began
+// in that CTA.  A thread sums four channels of every `parts`-th share; what it reads first is on its way while the shares'
+// references are compared.  And the outputs of requests without any row.
 constexpr int M_THREADS = 512, M_AHEAD = 6;
 template <typename T, int D, int GROUP>
-__global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, int ctas) {
+__global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P) {
   using C = RowsCfg<T, D, GROUP>;
-  extern __shared__ float m_smem[];                  // [ctas][G] factors; [M_THREADS] partial sums of four channels
+  extern __shared__ float m_smem[];                  // [CTAs][G] factors; [M_THREADS] partial sums of four channels
   __shared__ float s_top[8], s_sum[8];
   const CacheParams& c = P.c;
-  const int g = blockIdx.x, r = blockIdx.y, G = c.Hq / c.Hkv, lane = threadIdx.x & 31;
-  Requests<C::UNIT, C::TAIL> Q;
-  Q.read_all(c, P.n_req, lane);
+  const int G = c.Hq / c.Hkv, lane = threadIdx.x & 31, ctas = gridDim.x;
+  Requests<C::UNIT, C::TAIL> Q = {};
+  Q.read_all(c, P.n_req, lane, [&](int base) {
+    // no rows at all: an output of zero and a log-sum-exp of -inf, which merges into nothing
+    uint32_t none = __ballot_sync(0xffffffffu, base + lane < P.n_req && Q.units == 0 && (base + lane) % ctas == (int)blockIdx.x);
+    for (; threadIdx.x < 32 && none; none &= none - 1) {
+      const int64_t at = (int64_t)(base + __ffs(none) - 1) * c.Hq;
+      for (int i = lane; i < c.Hq * D; i += 32) narrow((T*)c.out + at * D + i, 0.f);
+      for (int i = lane; c.lse && i < c.Hq; i += 32) c.lse[at + i] = -CUDART_INF_F;
+    }
+  });
   const int total = Q.all * c.Hkv, per = per_cta(total, ctas);
-  int before = 0;
-  for (int base = 0; base < (r & ~31); base += 32) {
-    if (base) Q.read(c, P.n_req, base, lane);
-    before += __shfl_sync(0xffffffffu, Q.upto, 31);
-  }
-  if (r >= 32) Q.read(c, P.n_req, r & ~31, lane);
-  const int mine = __shfl_sync(0xffffffffu, Q.units, r & 31);
-  const int start = (before + __shfl_sync(0xffffffffu, Q.upto, r & 31) - mine) * c.Hkv + g * mine;
+  const int64_t next = ((int64_t)blockIdx.x + 1) * per;
+  Cursor<T, D, GROUP> pair = {};
+  if (next < total) pair.open(c, P.n_req, Q, (int)next, lane);
   // Every CTA waits, also one with nothing to do: the end of this kernel stands for the end of the one before.
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t at = (int64_t)r * c.Hq + g * G;
-  if (mine == 0) {
-    for (int i = threadIdx.x; i < G * D; i += M_THREADS) narrow((T*)c.out + at * D + i, 0.f);
-    if (c.lse && (int)threadIdx.x < G) c.lse[at + threadIdx.x] = -CUDART_INF_F;
-    return;
-  }
-  const int c0 = start / per, n = (start + mine - 1) / per - c0 + 1;
-  if (n == 1) return;
+  if (next >= total || pair.start == next || pair.start / per != (int)blockIdx.x) return;
+  const int64_t at = (int64_t)pair.r * c.Hq + pair.g * G;
+  const int c0 = blockIdx.x, n = (pair.start + pair.units - 1) / per - c0 + 1;
   // (the first CTA's share is the one at the end of its run)
   auto share = [&](int x) { return (int64_t)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * G; };
   const int quads = G * D / 4, parts = M_THREADS / quads, part = threadIdx.x / quads, quad = threadIdx.x % quads;
@@ -1014,7 +1020,7 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)P.c.Hkv, (unsigned)P.n_req, 1);
+  cfg.gridDim = dim3((unsigned)ctx->n_sm, 1, 1);
   cfg.blockDim = dim3(M_THREADS, 1, 1);
   cfg.dynamicSmemBytes = ((size_t)ctx->n_sm * (P.c.Hq / P.c.Hkv) + 3) / 4 * 16 + M_THREADS * 16;
   cfg.stream = st;
@@ -1023,17 +1029,18 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P, ctx->n_sm);
+  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P);
   count_launch(2);
   return e;
 }
 
 template <typename T, int D, int GROUP>
 cudaError_t run_rows(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
-  // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, 4-bit rows 12 x 2 of 2 to
-  // 6 KB (8 warps are as fast, 16 slower by 8 %: they have no more than 128 registers each); fp32 rows 3 x 2 of up to 32 KB.
+  // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, fp32 rows 3 x 2 of up to
+  // 32 KB, 4-bit rows of 128 channels 8 x 3 of 5 to 6 KB (12 x 2: 32 requests as fast, one request of 4096 rows 13.4 us instead of
+  // 12.8; 16 x 2, with 128 registers a thread, 8 % slower), of 64 channels 12 x 2 (8 x 3: 6 % slower).
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int W = GROUP ? (F32 ? 8 : 12) : F32 ? 3 : 4, ST = GROUP || F32 ? 2 : 3;
+  constexpr int W = !GROUP ? (F32 ? 3 : 4) : F32 || D == 128 ? 8 : 12, ST = (GROUP ? D == 128 && !F32 : !F32) ? 3 : 2;
   return P.c.Hq / P.c.Hkv <= 4 ? run_units<T, D, GROUP, true, W, ST>(ctx, P, st) : run_units<T, D, GROUP, false, W, ST>(ctx, P, st);
 }
 template <typename T>

@@ -613,3 +613,21 @@ def test_prompt_offsets_beyond_32_bits(layout):
     ref = small.accumulate_attention(qs, ks, want_lse)
     assert (one - ref).abs().max() <= 1e-5 * ref.abs().max()       # (few keys: their heads are split over CTAs)
     cake.destroy()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,d", [(5, 1, 64), (7, 1, 128), (10, 2, 128)])
+def test_prompt_groups_of_odd_size(hq, hkv, d, dtype):
+    lens = (150, 290)
+    cake = context(hq, hkv, d, dtype, lens, window=4)
+    check_prompt(cake, *prompt(hq, hkv, d, dtype, lens, seed=hq), lens, dtype, window=4)
+
+
+@pytest.mark.parametrize("group", [0, 32])
+def test_cache_thousands_of_requests(group):
+    """More requests than a warp reads at once, most of them short or empty."""
+    rng = np.random.default_rng(11)
+    lens = [int(n) for n in rng.integers(0, 4, size=3000)]
+    lens[2999] = 500
+    cake = context(2, 1, 64, BF16, layers=2)
+    check_cached(cake, cached(2, 1, 64, BF16, lens, group), BF16)
