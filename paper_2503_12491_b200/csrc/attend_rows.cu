@@ -919,21 +919,21 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   copy_wait<0>();
 }
 
-// Pairs that lie in several CTAs, from the shares these left: the pair that goes on from CTA blockIdx.x to the next, if it began
-// in that CTA.  A thread sums four channels of every `parts`-th share; what it reads first is on its way while the shares'
+// Pairs that lie in several CTAs, from the shares these left: a CTA per pair where there are fewer pairs than CTAs, else one per
+// boundary, for the pair that goes on from CTA blockIdx.x to the next, if it began in that CTA.  A thread sums four channels of every `parts`-th share; what it reads first is on its way while the shares'
 // references are compared.  And the outputs of requests without any row.
 constexpr int M_THREADS = 512, M_AHEAD = 6;
 template <typename T, int D, int GROUP>
-__global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P) {
+__global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, int ctas, bool by_pair) {
   using C = RowsCfg<T, D, GROUP>;
   extern __shared__ float m_smem[];                  // [CTAs][G] factors; [M_THREADS] partial sums of four channels
   __shared__ float s_top[8], s_sum[8];
   const CacheParams& c = P.c;
-  const int G = c.Hq / c.Hkv, lane = threadIdx.x & 31, ctas = gridDim.x;
+  const int G = c.Hq / c.Hkv, lane = threadIdx.x & 31;
   Requests<C::UNIT, C::TAIL> Q = {};
   Q.read_all(c, P.n_req, lane, [&](int base) {
     // no rows at all: an output of zero and a log-sum-exp of -inf, which merges into nothing
-    uint32_t none = __ballot_sync(0xffffffffu, base + lane < P.n_req && Q.units == 0 && (base + lane) % ctas == (int)blockIdx.x);
+    uint32_t none = __ballot_sync(0xffffffffu, base + lane < P.n_req && Q.units == 0 && (base + lane) % gridDim.x == blockIdx.x);
     for (; threadIdx.x < 32 && none; none &= none - 1) {
       const int64_t at = (int64_t)(base + __ffs(none) - 1) * c.Hq;
       for (int i = lane; i < c.Hq * D; i += 32) narrow((T*)c.out + at * D + i, 0.f);
@@ -941,14 +941,32 @@ __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P) {
     }
   });
   const int total = Q.all * c.Hkv, per = per_cta(total, ctas);
-  const int64_t next = ((int64_t)blockIdx.x + 1) * per;
   Cursor<T, D, GROUP> pair = {};
-  if (next < total) pair.open(c, P.n_req, Q, (int)next, lane);
+  bool mine;
+  if (by_pair) {
+    const int r = blockIdx.x / c.Hkv;
+    int before = 0;
+    for (int base = 0; base < r / 32 * 32; base += 32) {
+      before += __shfl_sync(0xffffffffu, Q.upto, 31);
+      Q.read(c, P.n_req, base + 32, lane);
+    }
+    pair.r = r; pair.g = blockIdx.x % c.Hkv;
+    pair.units = __shfl_sync(0xffffffffu, Q.units, r % 32);
+    pair.start = (before + __shfl_sync(0xffffffffu, Q.upto, r % 32) - pair.units) * c.Hkv + pair.g * pair.units;
+    mine = pair.units > 0 && pair.start / per != (pair.start + pair.units - 1) / per;
+  } else {
+    const int64_t next = ((int64_t)blockIdx.x + 1) * per;
+    mine = next < total;
+    if (mine) {
+      pair.open(c, P.n_req, Q, (int)next, lane);
+      mine = pair.start < next && pair.start / per == (int)blockIdx.x;
+    }
+  }
   // Every CTA waits, also one with nothing to do: the end of this kernel stands for the end of the one before.
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (next >= total || pair.start == next || pair.start / per != (int)blockIdx.x) return;
+  if (!mine) return;
   const int64_t at = (int64_t)pair.r * c.Hq + pair.g * G;
-  const int c0 = blockIdx.x, n = (pair.start + pair.units - 1) / per - c0 + 1;
+  const int c0 = pair.start / per, n = (pair.start + pair.units - 1) / per - c0 + 1;
   // (the first CTA's share is the one at the end of its run)
   auto share = [&](int x) { return (int64_t)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * G; };
   const int quads = G * D / 4, parts = M_THREADS / quads, part = threadIdx.x / quads, quad = threadIdx.x % quads;
@@ -1020,7 +1038,8 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctx->n_sm, 1, 1);
+  const bool by_pair = (int64_t)P.n_req * P.c.Hkv < ctx->n_sm;
+  cfg.gridDim = dim3((unsigned)(by_pair ? P.n_req * P.c.Hkv : ctx->n_sm), 1, 1);
   cfg.blockDim = dim3(M_THREADS, 1, 1);
   cfg.dynamicSmemBytes = ((size_t)ctx->n_sm * (P.c.Hq / P.c.Hkv) + 3) / 4 * 16 + M_THREADS * 16;
   cfg.stream = st;
@@ -1029,7 +1048,7 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P);
+  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P, ctx->n_sm, by_pair);
   count_launch(2);
   return e;
 }
