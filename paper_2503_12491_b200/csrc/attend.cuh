@@ -10,6 +10,34 @@ namespace cake {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2E = 1.4426950408889634f;
 
+// Programmatic dependent launch.  A kernel may take its places while the one before it in the stream ends, and touches global
+// memory only after after_previous(), which waits for all of that one's work; it lets the next one in only then, so that what
+// has run before its own predecessor is complete for whoever starts early behind it.
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+// Launches a kernel that way, as clusters of `cluster` CTAs.
+template <typename Kernel, typename... Args>
+cudaError_t launch_early(Kernel kernel, unsigned grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)cluster;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;              // (a cluster of one costs a CTA's turn more than none)
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Up to kPromptReqs requests of a batch, longest first, as a kernel parameter: a launch needs no table in device
 // memory, so a captured one stays valid whatever the context does next.
 constexpr int kPromptReqs = 128;

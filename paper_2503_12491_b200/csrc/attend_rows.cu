@@ -679,8 +679,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   Cursor<T, D, GROUP>* cursors = (Cursor<T, D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS + M::STATS + M::PLACES);
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
-  // merge_shares may take its places now; it waits for the end of this kernel before it reads anything of it
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_previous();                                  // (merge_shares may take its places now)
 
   // --- this CTA's units, and the pair of the first
   Requests<C::UNIT, C::TAIL> Q;
@@ -962,8 +961,9 @@ __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, in
       mine = pair.start < next && pair.start / per == (int)blockIdx.x;
     }
   }
-  // Every CTA waits, also one with nothing to do: the end of this kernel stands for the end of the one before.
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Every CTA waits, also one with nothing to do: the end of this kernel stands for the end of the one before.  (What is read
+  // up to here that one has read too, after all before it.)
+  after_previous();
   if (!mine) return;
   const int64_t at = (int64_t)pair.r * c.Hq + pair.g * G;
   const int c0 = pair.start / per, n = (pair.start + pair.units - 1) / per - c0 + 1;
@@ -1034,23 +1034,12 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
     if (e != cudaSuccess) return e;
     once.mark(ctx->device);
   }
-  kernel<<<(unsigned)ctx->n_sm, W * 32, M::BYTES, st>>>(P);
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_early(kernel, (unsigned)ctx->n_sm, W * 32, M::BYTES, 1, st, P);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
   const bool by_pair = (int64_t)P.n_req * P.c.Hkv < ctx->n_sm;
-  cfg.gridDim = dim3((unsigned)(by_pair ? P.n_req * P.c.Hkv : ctx->n_sm), 1, 1);
-  cfg.blockDim = dim3(M_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = ((size_t)ctx->n_sm * (P.c.Hq / P.c.Hkv) + 3) / 4 * 16 + M_THREADS * 16;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, merge_shares<T, D, GROUP>, P, ctx->n_sm, by_pair);
-  count_launch(2);
-  return e;
+  const size_t smem = ((size_t)ctx->n_sm * (P.c.Hq / P.c.Hkv) + 3) / 4 * 16 + M_THREADS * 16;
+  return launch_early(merge_shares<T, D, GROUP>, (unsigned)(by_pair ? P.n_req * P.c.Hkv : ctx->n_sm), M_THREADS, smem, 1, st, P, ctx->n_sm,
+                      by_pair);
 }
 
 template <typename T, int D, int GROUP>

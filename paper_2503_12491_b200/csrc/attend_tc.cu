@@ -201,6 +201,7 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *S.tmem;
+  after_previous();
   // Item i of the ring: K of tile 0, then V of tile j and K of tile j + 1 in turn.
   const int n_items = 2 * n_kv;
   auto stage_of = [](int i) { return i % C::STAGES; };
@@ -516,6 +517,7 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *S.tmem;
+  after_previous();
 
   if (warp == A_TMA) {
     mbar_expect_tx(S.k_full, TB);
@@ -670,9 +672,7 @@ static cudaError_t run_prompt_tc(const cake_ctx* ctx, const CUtensorMap& qm, con
     if (e != cudaSuccess) return e;
     once.mark(ctx->device);
   }
-  prompt_tc<D><<<(unsigned)(B.tiles * P.Hq), P_THREADS, PromptCfg<D>::SMEM, st>>>(qm, km, vm, B, P);
-  count_launch();
-  return cudaGetLastError();
+  return launch_early(prompt_tc<D>, (unsigned)(B.tiles * P.Hq), P_THREADS, PromptCfg<D>::SMEM, 1, st, qm, km, vm, B, P);
 }
 
 int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const void* v, void* out, Strided os,
@@ -707,21 +707,8 @@ static cudaError_t run_accumulate_tc(const cake_ctx* ctx, const CUtensorMap& qm,
     if (e != cudaSuccess) return e;
     once.mark(ctx->device);
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(B.tiles * (kSplit ? P.Hq : P.Hkv)), 1, 1);
-  cfg.blockDim = dim3(A_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = acc_smem<D>();
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)P.G;          // (at most 8: portable)
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = kSplit ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, accumulate_tc<D, kSplit>, qm, km, B, P);
-  count_launch();
-  return e;
+  return launch_early(accumulate_tc<D, kSplit>, (unsigned)(B.tiles * (kSplit ? P.Hq : P.Hkv)), A_THREADS, acc_smem<D>(), kSplit ? P.G : 1,
+                      st, qm, km, B, P);               // (G is at most 8: portable)
 }
 
 int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, const void* k, const float* lse, float* out,

@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  after_previous();
   if (warp < 4) {
     const int key = key0 + warp * 32 + lane;
     put_row<D>(P.k + (g * P.T + cu + key) * D, key < N, tmem + ((uint32_t)(warp * 32) << 16) + A_KEYS);
@@ -351,6 +352,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  after_previous();
   constexpr int DH = D / 2;                      // channels of an output thread
   float o[DH];                                   // (warps 4 to 11)
 #pragma unroll
@@ -553,20 +555,7 @@ int32_t run32(const cake_ctx* ctx, const Tc32Params& P, cudaStream_t st) {
   PromptBatch B;
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {
     fill_prompt_batch(ctx, lo, TILE, B);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(B.tiles * P.Hq), 1, 1);
-    cfg.blockDim = dim3(kPrompt ? P_THREADS : A_THREADS, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = kPrompt ? 1 : (unsigned)P.G;        // (at most 8: portable)
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    CAKE_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, B, P));
-    count_launch();
+    CAKE_CUDA_TRY(launch_early(kernel, (unsigned)(B.tiles * P.Hq), kPrompt ? P_THREADS : A_THREADS, smem, kPrompt ? 1 : P.G, st, B, P));
   }
   return CAKE_OK;
 }
