@@ -9,6 +9,8 @@ namespace cake {
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2E = 1.4426950408889634f;
+// Reference of a row of which no logit above -inf has come yet: those are then weighed as 0 beside later ones, not as NaN.
+constexpr float kNoWeight = -3.402823466e38f;
 
 // Programmatic dependent launch.  A kernel may take its places while the one before it in the stream ends, and touches global
 // memory only after after_previous(), which waits for all of that one's work; it lets the next one in only then, so that what
@@ -79,7 +81,7 @@ struct CacheParams {
   void* out;
   float* lse;
   int n_layers, layer, Hq, Hkv, group;
-  float scale2, scale;
+  float scale2;
 };
 
 // attend_rows.cu

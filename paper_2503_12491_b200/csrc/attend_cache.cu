@@ -27,7 +27,6 @@ int32_t common_args(const cake_ctx* ctx, int32_t n_req, int32_t layer, const voi
   P.q = q; P.row_off = row_offsets; P.out = out;
   if (tail_capacity > 0) { P.k_tail = k_tail; P.v_tail = v_tail; P.tail_len = tail_len; P.tail_cap = tail_capacity; }
   P.n_layers = c.n_layers; P.layer = layer; P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads;
-  P.scale = 1.f / sqrtf((float)c.head_dim);
   P.scale2 = kLog2E / sqrtf((float)c.head_dim);
   return CAKE_OK;
 }

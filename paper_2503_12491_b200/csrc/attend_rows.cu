@@ -178,7 +178,7 @@ struct Running {
   float ref[2], sum[2], o[D / 16][4];
   f32x2 z[(NG + 1) / 2];
   __device__ __forceinline__ void clear() {
-    ref[0] = ref[1] = -CUDART_INF_F;
+    ref[0] = ref[1] = kNoWeight;
     sum[0] = sum[1] = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
@@ -531,7 +531,7 @@ struct Running32 {
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
-      ref[h] = -CUDART_INF_F;
+      ref[h] = kNoWeight;
       sum[h] = 0.f;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) o[h][c] = 0.f;

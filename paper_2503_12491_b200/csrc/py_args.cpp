@@ -467,6 +467,10 @@ Tail tail_of(PyObject* const* a, at::ScalarType e, int64_t n_req, int64_t hkv, i
   return t;
 }
 
+// Start of a part of a cache.  One without rows (all requests have tails alone) has no memory: it is never read, and anything
+// stands for it.
+const void* rows_of(const at::Tensor& t, const at::Tensor& stand_in) { return t.numel() ? t.data_ptr() : stand_in.data_ptr(); }
+
 // attend_cache(ctx, is_fp32, layer, n_layers, q_heads, kv_heads, head_dim, q, row_offsets, k_tail, v_tail, tail_len, out, lse,
 //              k_cache, v_cache)
 // attend_int4(the same up to lse, k_codes, k_scale, k_zero, v_codes, v_scale, v_zero, kgroup_offsets)
@@ -489,7 +493,7 @@ PyObject* attend_cached(PyObject* const* a, bool int4) {
     if (!int4) {
       const at::Tensor &k = tensor(a[14], "k_cache", e, {-1, d}), &v = tensor(a[15], "v_cache", e, {-1, d});
       rc = released([&](void* st) {
-        return lib.attend_cache(c, (int32_t)R, (int32_t)layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), off, t.k, t.v, t.len, t.cap,
+        return lib.attend_cache(c, (int32_t)R, (int32_t)layer, q.data_ptr(), rows_of(k, ws), rows_of(v, ws), off, t.k, t.v, t.len, t.cap,
                                 out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes, st);
       });
     } else {
@@ -499,9 +503,9 @@ PyObject* attend_cached(PyObject* const* a, bool int4) {
       const int64_t* koff = (const int64_t*)tensor(a[20], "kgroup_offsets", i64, {R * L + 1}).data_ptr();
       if (vs.size(1) < 1 || d % vs.size(1)) throw std::invalid_argument("v_scale: no such group");
       rc = released([&](void* st) {
-        return lib.attend_int4(c, (int32_t)R, (int32_t)layer, q.data_ptr(), (const uint8_t*)kc.data_ptr(), (const float*)ks.data_ptr(),
-                               (const float*)kz.data_ptr(), (const uint8_t*)vc.data_ptr(), (const float*)vs.data_ptr(),
-                               (const float*)vz.data_ptr(), (int32_t)(d / vs.size(1)), off, koff, t.k, t.v, t.len, t.cap,
+        return lib.attend_int4(c, (int32_t)R, (int32_t)layer, q.data_ptr(), (const uint8_t*)rows_of(kc, ws), (const float*)rows_of(ks, ws),
+                               (const float*)rows_of(kz, ws), (const uint8_t*)rows_of(vc, ws), (const float*)rows_of(vs, ws),
+                               (const float*)rows_of(vz, ws), (int32_t)(d / vs.size(1)), off, koff, t.k, t.v, t.len, t.cap,
                                out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes, st);
       });
     }

@@ -631,3 +631,90 @@ def test_cache_thousands_of_requests(group):
     lens[2999] = 500
     cake = context(2, 1, 64, BF16, layers=2)
     check_cached(cake, cached(2, 1, 64, BF16, lens, group), BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
+def test_cache_logits_of_minus_infinity(dtype):
+    """Keys whose logit is -inf weigh nothing, also where a whole unit of rows has no other; only a request of such keys alone has
+    no answer."""
+    lens, d = (200, 33, 5), 64
+    x = cached(4, 2, d, dtype, lens, seed=9)
+    x["q"][:, :, 0] = 1
+    bad = [np.r_[0:64, 100:140, 199], np.r_[32], np.r_[0:5]]
+    for r, n in enumerate(lens):
+        for g in range(2):
+            x["k"][int(x["offn"][r * 2 + 1]) + g * n + torch.from_numpy(bad[r]).cuda(), 0] = float("-inf")
+    out, lse = run_cached(context(4, 2, d, dtype, layers=2), x)
+    assert torch.isnan(out[2]).all() and (lse[2] == float("-inf")).all()
+    on, ln, qn = f64(out), f64(lse), f64(x["q"])
+    for r, n in enumerate(lens[:2]):
+        for g in range(2):
+            keep = int(x["offn"][r * 2 + 1]) + g * n + np.setdiff1d(np.arange(n), bad[r])
+            k, v, heads = x["kn"][keep], x["vn"][keep], slice(2 * g, 2 * g + 2)
+            check_out(on[r, heads], ln[r, heads], O.attend(qn[r, heads], k, v), weight_error(qn[r, heads], k, d), n, dtype)
+
+
+def test_prompt_logits_of_minus_infinity():
+    n, bad, d = 700, 270, 64
+    cake = context(2, 1, d, BF16, (n,))
+    q, k, v = prompt(2, 1, d, BF16, (n,), seed=4)
+    q[:, :, 0] = 1
+    k[:, :bad, 0] = float("-inf")
+    out, lse = cake.attend_prompt(q, k, v)
+    assert torch.isnan(out[:, :bad]).all() and (lse[:, :bad] == float("-inf")).all()
+    qn, kn, vn = f64(q[:, bad:]), f64(k[:, bad:]), f64(v[:, bad:])
+    check_out(f64(out[:, bad:]), f64(lse[:, bad:]), O.prompt_attention(qn, kn, vn), weight_error(qn, kn, d), n, BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("group", [0, 32])
+def test_cache_of_tails_alone(dtype, group):
+    """No packed row at all: the cache's tensors have no memory."""
+    cake = context(4, 2, 64, dtype, layers=1)
+    x = cached(4, 2, 64, dtype, (0, 0), group=group, tail=(7, np.array([7, 3])), layers=1, layer=0)
+    if group:
+        x["cache"] = {n: t if n.endswith("offsets") else t[:0] for n, t in x["cache"].items()}
+        x["cache"] = {n: t if n.endswith("offsets") else torch.empty_like(t) for n, t in x["cache"].items()}
+    else:
+        x["k"], x["v"] = (torch.empty((0, 64), dtype=dtype, device="cuda") for _ in range(2))
+    check_cached(cake, x, dtype)
+
+
+@pytest.mark.parametrize("group", [0, 32])
+def test_calls_among_copies_and_other_streams_in_a_graph(group):
+    """A captured step whose kernels follow copies, a fill and a join of two streams, several times behind one another: the same
+    as one by one, whatever of it may start early."""
+    lens = (700, 40)
+    cake = context(8, 2, 128, BF16, lens, layers=2)
+    q, k, v = prompt(8, 2, 128, BF16, lens, seed=2)
+    x = cached(8, 2, 128, BF16, (900, 130, 33), group=group, tail=(9, np.array([9, 0, 4])), seed=8)
+    queries = x["q"].clone()
+
+    def step(side):
+        main = torch.cuda.current_stream()
+        got = []
+        lse = torch.zeros(8, sum(lens), device="cuda")
+        x["q"].copy_(queries)
+        got += run_cached(cake, x)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            first = cake.attend_prompt(q, k, v, lse=lse)
+            received = cake.accumulate_attention(q, k, lse)
+        x["q"].mul_(0.5)
+        got += run_cached(cake, x)
+        main.wait_stream(side)
+        got += run_cached(cake, x)
+        got += [first[0], lse, received, cake.accumulate_attention(q, k, lse)]
+        return got
+
+    side = torch.cuda.Stream()
+    want = [t.clone() for t in step(side)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(side)
+    for _ in range(3):
+        for t in got:
+            t.fill_(7)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
