@@ -50,6 +50,8 @@ template <typename T, int D, int GROUP> struct RowsCfg {
 struct RowsParams {
   CacheParams c;
   float* shares;                                 // [CTA][2][G][D], then [CTA][2][G][2] (reference, sum)
+  int32_t* status;
+  long long limit;                               // cycles that a wait may take
   int n_req;
 };
 __host__ __device__ inline int64_t share_stats(int ctas, int G, int D) { return (int64_t)ctas * 2 * G * D; }
@@ -154,6 +156,43 @@ struct Cursor {
 
 __device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
 __device__ __forceinline__ void narrow(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+// Two or four consecutive numbers, from shared memory and to where they are stored.
+__device__ __forceinline__ void ld_floats(float (&x)[2], const float* p) { const float2 a = *reinterpret_cast<const float2*>(p); x[0] = a.x; x[1] = a.y; }
+__device__ __forceinline__ void ld_floats(float (&x)[4], const float* p) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+}
+__device__ __forceinline__ void st_row(float* p, const float (&x)[2]) { *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]); }
+__device__ __forceinline__ void st_row(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void st_row(__nv_bfloat16* p, const float (&x)[2]) { *reinterpret_cast<uint32_t*>(p) = bf16_pair(x[0], x[1]); }
+__device__ __forceinline__ void st_row(__nv_bfloat16* p, const float (&x)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+}
+
+// Counters in shared memory through which warps hand results to one another.
+__device__ __forceinline__ int add_count(int* p) {
+  int old;
+  asm volatile("atom.acq_rel.cta.shared::cta.add.s32 %0, [%1], 1;" : "=r"(old) : "r"(smem_addr(p)) : "memory");
+  return old;
+}
+__device__ __forceinline__ void set_count(int* p, int n) {
+  asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_addr(p)), "r"(n) : "memory");
+}
+// Until the counter is at least n, by every lane; false after `limit` cycles.
+__device__ __forceinline__ bool wait_count(const int* p, int n, int32_t* status, long long limit) {
+  const long long t0 = clock64();
+  for (;;) {
+    int x;
+    asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(x) : "r"(smem_addr(p)) : "memory");
+    const bool there = x >= n;
+    if (__all_sync(0xffffffffu, there)) return true;
+    const bool late = clock64() - t0 > limit;
+    if (__any_sync(0xffffffffu, late)) {
+      atomicCAS(status, 0, CAKE_ERR_TIMEOUT);
+      return false;
+    }
+  }
+}
 
 __device__ __forceinline__ float ex2a(float x) {
   float y;
@@ -165,10 +204,14 @@ template <typename T, int D, int GROUP, bool kTwo, int W, int ST>
 struct RowsSmem {
   using C = RowsCfg<T, D, GROUP>;
   static constexpr int HEADS = kTwo ? 4 : 8, PK = 36;                            // floats of a head's weights of a unit (padded)
-  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * (HEADS * PK + (C::F32 ? HEADS * D : 0)) * 4, STATS = (size_t)(W + 1) * HEADS * 8,
-                          PLACES = (size_t)W * 8, CURSORS = (size_t)W * sizeof(Cursor<T, D, GROUP>);
-  static constexpr size_t BYTES = RING + WEIGHTS + STATS + PLACES + CURSORS;
-  static_assert(C::STAGE >= HEADS * (D + C::NG) * 4, "a warp's results fit a stage");
+  // a warp's results of a pair: outputs [head][channel], sums of weights times zeros [head][group], (reference, sum) [head]
+  static constexpr int ZEROS = HEADS * D, STATS = ZEROS + HEADS * C::NG, RESULT = (STATS + 2 * HEADS + 3) / 4 * 4;
+  static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * (HEADS * PK + (C::F32 ? HEADS * D : 0)) * 4,
+                          CURSORS = (size_t)W * sizeof(Cursor<T, D, GROUP>), RESULTS = (size_t)W * RESULT * 4;
+  // places for all warps' results of a pair: two if they fit
+  static constexpr int PLACES = RING + WEIGHTS + CURSORS + 2 * RESULTS + 16 <= 227 * 1024 ? 2 : 1;
+  static constexpr size_t BYTES = RING + WEIGHTS + CURSORS + PLACES * RESULTS + 16;
+  static_assert(C::STAGE >= RESULT * 4 && WEIGHTS % 16 == 0 && CURSORS % 16 == 0, "a warp's results fit a stage; 16-byte pieces");
 };
 
 // A warp's running softmax: reference and (this lane's part of the) sum of the two heads of its columns 2 j, 2 j + 1, outputs
@@ -673,12 +716,13 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* ring = smem_raw;
   float* weights = (float*)(smem_raw + M::RING);
-  float2* m_stat = (float2*)(smem_raw + M::RING + M::WEIGHTS);
-  float2* m_total = m_stat + W * HEADS;
-  int* m_place = (int*)(smem_raw + M::RING + M::WEIGHTS + M::STATS);             // where a warp's results lie in the ring
-  Cursor<T, D, GROUP>* cursors = (Cursor<T, D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS + M::STATS + M::PLACES);
+  Cursor<T, D, GROUP>* cursors = (Cursor<T, D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS);
+  float* results = (float*)(smem_raw + M::RING + M::WEIGHTS + M::CURSORS);       // [place][warp][RESULT]
+  int *arrived = (int*)(results + M::PLACES * W * M::RESULT), *merged = arrived + 2;     // per place
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
+  if (threadIdx.x < 4) arrived[threadIdx.x] = 0;
+  __syncthreads();
   after_previous();                                  // (merge_shares may take its places now)
 
   // --- this CTA's units, and the pair of the first
@@ -732,18 +776,22 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   const int n = lane >> 2, j = lane & 3, head = kTwo ? n & 3 : n;
   float* sp = weights + warp * HEADS * PK;
   float* qs = weights + W * HEADS * PK + warp * HEADS * D;                       // (fp32: queries)
-  int k = 0;
-  for (int u = u0; u < u1; ) {                   // pair by pair
+  int k = 0, shared = 0;                             // this warp's units so far; pairs so far that several warps had
+  for (int u = u0, end; u < u1; u = end) {           // pair by pair
     work.seek(c, P.n_req, u);
-    const int end = min(work.start + work.units, u1), packed = (int)((work.len.n + C::UNIT - 1) / C::UNIT);
-    // --- the pair ends here (or this CTA's part of it): the warps' results together, each in the one stage of its ring that
-    // holds no unit to come
-    int place;
-    float* m_out;
+    end = min(work.start + work.units, u1);
+    const int packed = (int)((work.len.n + C::UNIT - 1) / C::UNIT);
+    // the warps that have units of it, from warp `head_warp` on in turn
+    const int parts = min(W, end - u), head_warp = (u - u0) % W;
+    const int place = shared % M::PLACES, before = shared / M::PLACES;
+    if (parts > 1) ++shared;
+    if ((warp + W - head_warp) % W >= parts) continue;
+    // Where its results go: by itself a warp takes the one stage of its ring that holds no unit to come, otherwise its part of a
+    // place whose last pair has been put together.
+    float* mine;
     auto open_place = [&]() {
-      place = (warp * ST + (k + ST - 1) % ST) * C::STAGE;
-      m_out = (float*)(ring + place);
-      if (lane == 0) m_place[warp] = place;
+      mine = parts == 1 ? (float*)(my_ring + (size_t)((k + ST - 1) % ST) * C::STAGE) : results + (place * W + warp) * M::RESULT;
+      return parts == 1 || wait_count(merged + place, before, P.status, P.limit);
     };
     if constexpr (C::F32) {
       Running32<D, HEADS> R;
@@ -780,14 +828,14 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           dense32_unit<D, HEADS, C::TAIL>(R, qs, st, st + C::TAIL * D * 4, valid, c.scale2, sp, lane);
         }
       }
-      open_place();
+      if (!open_place()) break;
 #pragma unroll
       for (int h = 0; h < HEADS; ++h) {
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) R.sum[h] += __shfl_xor_sync(0xffffffffu, R.sum[h], x);
-        if (lane == 0) m_stat[warp * HEADS + h] = make_float2(R.ref[h], R.sum[h]);
+        if (lane == 0) *reinterpret_cast<float2*>(mine + M::STATS + 2 * h) = make_float2(R.ref[h], R.sum[h]);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) m_out[h * D + lane * (D / 32) + i] = R.o[h][i];
+        for (int i = 0; i < D / 32; ++i) mine[h * D + lane * (D / 32) + i] = R.o[h][i];
       }
     } else {
       Running<D, NG> R;
@@ -837,15 +885,14 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           }
         }
       }
-      open_place();
+      if (!open_place()) break;
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) {
         R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
         R.sum[1] += __shfl_xor_sync(0xffffffffu, R.sum[1], x);
       }
       if (n == 0 && (!kTwo || j < 2)) {
-        m_stat[warp * HEADS + 2 * j] = make_float2(R.ref[0], R.sum[0]);
-        m_stat[warp * HEADS + 2 * j + 1] = make_float2(R.ref[1], R.sum[1]);
+        *reinterpret_cast<float4*>(mine + M::STATS + 4 * j) = make_float4(R.ref[0], R.sum[0], R.ref[1], R.sum[1]);
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
@@ -855,7 +902,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         for (int e = 0; e < 4; ++e) {
           float x = R.o[i][e];
           if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 2);
-          if (!kTwo || j < 2) m_out[(2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
+          if (!kTwo || j < 2) mine[(2 * j + (e & 1)) * D + (e >> 1 ? ch1 : ch0)] = x;
         }
       }
       if constexpr (C::INT4) {
@@ -867,53 +914,76 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           x += __shfl_xor_sync(0xffffffffu, x, 1);
           x += __shfl_xor_sync(0xffffffffu, x, 2);
           if (kTwo) x += __shfl_xor_sync(0xffffffffu, x, 16);
-          if (j == 0 && (!kTwo || n < 4)) m_out[HEADS * D + head * NG + i] = x;
+          if (j == 0 && (!kTwo || n < 4)) mine[M::ZEROS + head * NG + i] = x;
         }
       }
     }
-    __syncthreads();
-    // every warp's factor to the largest reference of its head (in place of the reference)
-    for (int h = warp; h < G; h += W) {
-      float2 t = lane < W ? m_stat[lane * HEADS + h] : make_float2(-CUDART_INF_F, 0.f);
-      float top = t.x;
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      const float f = t.y == 0.f ? 0.f : exp2f(t.x - top);      // (a warp without units of this pair)
-      float sum = t.y * f;
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      if (lane < W) m_stat[lane * HEADS + h].x = f;
-      if (lane == 0) m_total[h] = make_float2(top, sum);
+    // --- the warp that comes last puts the results together, in their order; nobody waits for it
+    __syncwarp();
+    if (parts > 1) {
+      int last = 0;
+      if (lane == 0) last = add_count(arrived + place) == parts - 1;
+      if (!__shfl_sync(0xffffffffu, last, 0)) continue;
     }
-    __syncthreads();
+    const float* of = parts == 1 ? mine - warp * M::RESULT : results + place * W * M::RESULT;      // warp w's at w * RESULT
     const bool whole = work.start >= u0 && work.start + work.units <= u1;
-    const int64_t share = (int64_t)blockIdx.x * 2 + (work.start >= u0 ? 1 : 0);
-    for (int i = threadIdx.x; i < G * D; i += W * 32) {
-      const int h = i / D, ch = i % D;
-      float acc = 0.f;
+    const int64_t share = (int64_t)blockIdx.x * 2 + (work.start >= u0 ? 1 : 0), at = (int64_t)work.r * c.Hq + work.g * G;
+    // a lane per warp and head: the warp's factor to the head's largest reference, the head's sum
+    constexpr int PW = W <= 4 ? 4 : W <= 8 ? 8 : 16, HP = 32 / PW, PASSES = HEADS > HP ? HEADS / HP : 1;
+    const int w0 = lane % PW;
+    const bool has = w0 < W && (w0 + W - head_warp) % W < parts;
+    const uint32_t live = __ballot_sync(0xffffffffu, has);
+    float f[PASSES], top[PASSES], sum[PASSES];
+#pragma unroll
+    for (int x = 0; x < PASSES; ++x) {
+      const int h = x * HP + lane / PW;
+      const float2 t = has && h < G ? *reinterpret_cast<const float2*>(of + w0 * M::RESULT + M::STATS + 2 * h) : make_float2(kNoWeight, 0.f);
+      top[x] = t.x;
+#pragma unroll
+      for (int y = PW / 2; y > 0; y >>= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], y));
+      f[x] = ex2a(t.x - top[x]);
+      sum[x] = t.y * f[x];
+#pragma unroll
+      for (int y = PW / 2; y > 0; y >>= 1) sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], y);
+    }
+    constexpr int CL = D / 32;                       // channels of a lane
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      if (h >= G) break;
+      float acc[CL] = {};
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float* of = (const float*)(ring + m_place[w]);
-        float x = of[h * D + ch];
-        if constexpr (C::INT4 && !C::F32) x += of[HEADS * D + h * NG + ch / GROUP];
-        acc = fmaf(x, m_stat[w * HEADS + h].x, acc);
-      }
-      const float top = m_total[h].x, sum = m_total[h].y;
-      if (whole) {
-        const int64_t at = (int64_t)work.r * c.Hq + work.g * G + h;
-        narrow((T*)c.out + at * D + ch, acc / sum);
-        if (c.lse && ch == 0) c.lse[at] = (top + log2f(sum)) * kLn2;
-      } else {
-        P.shares[(share * G + h) * D + ch] = acc;
-        if (ch == 0) {
-          float* st = P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2;
-          st[0] = top;
-          st[1] = sum;
+        const float fw = __shfl_sync(0xffffffffu, f[h / HP], h % HP * PW + w);
+        if (live >> w & 1) {
+          const float* from = of + w * M::RESULT;
+          float x[CL];
+          ld_floats(x, from + h * D + lane * CL);
+          if constexpr (C::INT4 && !C::F32) {
+            const float z = from[M::ZEROS + h * NG + lane * CL / GROUP];
+#pragma unroll
+            for (int e = 0; e < CL; ++e) x[e] += z;
+          }
+#pragma unroll
+          for (int e = 0; e < CL; ++e) acc[e] = fmaf(x[e], fw, acc[e]);
         }
       }
+      const float top_h = __shfl_sync(0xffffffffu, top[h / HP], h % HP * PW), sum_h = __shfl_sync(0xffffffffu, sum[h / HP], h % HP * PW);
+      if (whole) {
+        const float inv = 1.f / sum_h;
+#pragma unroll
+        for (int e = 0; e < CL; ++e) acc[e] *= inv;
+        st_row((T*)c.out + (at + h) * D + lane * CL, acc);
+        if (c.lse && lane == 0) c.lse[at + h] = (top_h + log2f(sum_h)) * kLn2;
+      } else {
+        st_row(P.shares + (share * G + h) * D + lane * CL, acc);
+        if (lane == 0) *reinterpret_cast<float2*>(P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2) = make_float2(top_h, sum_h);
+      }
     }
-    __syncthreads();
-    u = end;
+    __syncwarp();
+    if (parts > 1 && lane == 0) {
+      arrived[place] = 0;
+      set_count(merged + place, before + 1);
+    }
   }
   copy_wait<0>();
 }
@@ -1073,6 +1143,8 @@ int32_t launch_rows(const cake_ctx* ctx, int32_t n_req, const CacheParams& c, vo
   RowsParams P;
   P.c = c;
   P.shares = (float*)workspace;
+  P.status = ctx->d_status;
+  P.limit = ctx->wait_limit_cycles > 0 ? ctx->wait_limit_cycles : kSpinLimit;
   P.n_req = n_req;
   return cuda_status(ctx->cfg.dtype == CAKE_DTYPE_FP32 ? run_typed<float>(ctx, P, st) : run_typed<__nv_bfloat16>(ctx, P, st));
 }
