@@ -928,55 +928,64 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     const float* of = parts == 1 ? mine - warp * M::RESULT : results + place * W * M::RESULT;      // warp w's at w * RESULT
     const bool whole = work.start >= u0 && work.start + work.units <= u1;
     const int64_t share = (int64_t)blockIdx.x * 2 + (work.start >= u0 ? 1 : 0), at = (int64_t)work.r * c.Hq + work.g * G;
-    // a lane per warp and head: the warp's factor to the head's largest reference, the head's sum
-    constexpr int PW = W <= 4 ? 4 : W <= 8 ? 8 : 16, HP = 32 / PW, PASSES = HEADS > HP ? HEADS / HP : 1;
+    // a lane per warp and head: the warp's factor to the head's largest reference, that and the head's sum; they go where the weights
+    // were.  (Short loops: code that runs once per pair is not in the instruction cache.)
+    constexpr int PW = W <= 4 ? 4 : W <= 8 ? 8 : 16, HP = 32 / PW;
+    static_assert(HEADS * (PW + 2) <= HEADS * PK, "room");
+    float2* of_head = reinterpret_cast<float2*>(sp + HEADS * PW);
     const int w0 = lane % PW;
     const bool has = w0 < W && (w0 + W - head_warp) % W < parts;
     const uint32_t live = __ballot_sync(0xffffffffu, has);
-    float f[PASSES], top[PASSES], sum[PASSES];
-#pragma unroll
-    for (int x = 0; x < PASSES; ++x) {
-      const int h = x * HP + lane / PW;
+#pragma unroll 1
+    for (int h = lane / PW; h < (HEADS > HP ? HEADS : HP); h += HP) {            // (whole warps)
       const float2 t = has && h < G ? *reinterpret_cast<const float2*>(of + w0 * M::RESULT + M::STATS + 2 * h) : make_float2(kNoWeight, 0.f);
-      top[x] = t.x;
+      float top = t.x;
 #pragma unroll
-      for (int y = PW / 2; y > 0; y >>= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], y));
-      f[x] = ex2a(t.x - top[x]);
-      sum[x] = t.y * f[x];
+      for (int y = PW / 2; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+      const float f = ex2a(t.x - top);
+      float sum = t.y * f;
 #pragma unroll
-      for (int y = PW / 2; y > 0; y >>= 1) sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], y);
+      for (int y = PW / 2; y > 0; y >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
+      if (h < HEADS) {
+        sp[h * PW + w0] = f;
+        if (w0 == 0) of_head[h] = make_float2(top, sum);
+      }
     }
+    __syncwarp();
     constexpr int CL = D / 32;                       // channels of a lane
+#pragma unroll 1
+    for (int h = 0; h < G; ++h) {
+      // (all loads first, so that they are on their way together)
+      float x[W][CL], z[W], f[PW], acc[CL] = {};
 #pragma unroll
-    for (int h = 0; h < HEADS; ++h) {
-      if (h >= G) break;
-      float acc[CL] = {};
+      for (int w = 0; w < W; w += 4) {
+        const float4 y = *reinterpret_cast<const float4*>(sp + h * PW + w);
+        f[w] = y.x; f[w + 1] = y.y; f[w + 2] = y.z; f[w + 3] = y.w;
+      }
+      const float2 total = of_head[h];
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float fw = __shfl_sync(0xffffffffu, f[h / HP], h % HP * PW + w);
+#pragma unroll
+        for (int e = 0; e < CL; ++e) x[w][e] = 0.f;
+        z[w] = 0.f;
         if (live >> w & 1) {
-          const float* from = of + w * M::RESULT;
-          float x[CL];
-          ld_floats(x, from + h * D + lane * CL);
-          if constexpr (C::INT4 && !C::F32) {
-            const float z = from[M::ZEROS + h * NG + lane * CL / GROUP];
-#pragma unroll
-            for (int e = 0; e < CL; ++e) x[e] += z;
-          }
-#pragma unroll
-          for (int e = 0; e < CL; ++e) acc[e] = fmaf(x[e], fw, acc[e]);
+          ld_floats(x[w], of + w * M::RESULT + h * D + lane * CL);
+          if constexpr (C::INT4 && !C::F32) z[w] = of[w * M::RESULT + M::ZEROS + h * NG + lane * CL / GROUP];
         }
       }
-      const float top_h = __shfl_sync(0xffffffffu, top[h / HP], h % HP * PW), sum_h = __shfl_sync(0xffffffffu, sum[h / HP], h % HP * PW);
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int e = 0; e < CL; ++e) acc[e] = fmaf(x[w][e] + z[w], f[w], acc[e]);
       if (whole) {
-        const float inv = 1.f / sum_h;
+        const float inv = 1.f / total.y;
 #pragma unroll
         for (int e = 0; e < CL; ++e) acc[e] *= inv;
         st_row((T*)c.out + (at + h) * D + lane * CL, acc);
-        if (c.lse && lane == 0) c.lse[at + h] = (top_h + log2f(sum_h)) * kLn2;
+        if (c.lse && lane == 0) c.lse[at + h] = (total.x + log2f(total.y)) * kLn2;
       } else {
         st_row(P.shares + (share * G + h) * D + lane * CL, acc);
-        if (lane == 0) *reinterpret_cast<float2*>(P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2) = make_float2(top_h, sum_h);
+        if (lane == 0) *reinterpret_cast<float2*>(P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2) = total;
       }
     }
     __syncwarp();
