@@ -326,7 +326,7 @@ int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t
  * 1 / sqrt(d).  Softmax statistics, sums and outputs are held in fp32 and rounded once at the end.
  * These calls do not advance the context's batch: they may come at any point of it, on any stream, and
  * several times.  They allocate nothing, synchronise nothing, and a stream capture may record them.  A bounded wait
- * that runs out in a kernel over prompts shows in cake_status as CAKE_ERR_TIMEOUT, as elsewhere.
+ * that runs out in one of their kernels shows in cake_status as CAKE_ERR_TIMEOUT, as elsewhere.
  * Tensors must start on 16-byte boundaries, and the context's device must be the current one, else
  * CAKE_ERR_ARG. */
 

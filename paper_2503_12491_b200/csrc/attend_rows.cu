@@ -7,11 +7,13 @@
 // a unit in the 4-bit kernel, whose stages are smaller), and every CTA of one per SM takes the same number of consecutive
 // units, whatever pairs they belong to: the device works evenly on ragged batches, and on one long request.  Lengths lie on
 // the device, so each CTA adds up the units of all requests for itself.  Inside a CTA the warps take the units in turn, each
-// with copies of its own units in flight (cp.async) and its own running softmax; they meet only where a pair ends.  A pair that
-// lies in one CTA is finished there; of the others a CTA leaves its share in the workspace (at most one share at either end
+// with copies of its own units in flight (cp.async) and its own running softmax.  Where a pair ends they leave their results in one
+// of two places in turn, without waiting, and the first warp that wants the place again puts them together: the one that is
+// ahead.  (With a barrier at each end 256 requests of 560 rows in 4 bits took 131 us, where this takes 109; the last warp
+// doing it, which is the one behind, 117.)  A pair that lies in one CTA is finished there; of the others a CTA leaves its share in the workspace (at most one share at either end
 // of its run), and merge_shares, a CTA per boundary between two runs, puts them together: no CTA waits for another, and the
 // workspace needs no initialisation.  (In one launch instead: by clusters of 16 CTAs per head 11.2 us for one request of 2048 rows
-// and 8 heads, where this takes 8.0; by the CTA that leaves a pair's last share, counted with atomics, 16.4.)
+// and 8 heads, where this takes 8.6; by the CTA that leaves a pair's last share, counted with atomics, 16.4.)
 //
 // bf16 queries: products on the tensor cores (mma m16n8k16).  S^T[key][col] = K Q^T and O^T[channel][col] = V^T P^T with the
 // query heads as the 8 columns.  With up to four heads the columns 4 to 7 hold the same heads once more, for the second term of
@@ -26,9 +28,9 @@
 // pace).  Channels and keys are taken in whatever order the words bring them, the same one in both operands; a value tile's 16
 // channels come from one group of 32, which has one scale per row.
 //
-// Bound.  bf16 and fp32 rows: DRAM, 5.9 TB/s of the 6.5 that a copy reaches (32 requests of 1000 to 6000 rows, 8 heads).  4-bit
+// Bound.  bf16 and fp32 rows: DRAM, 5.9 TB/s of the 6.5 that a copy reaches (76 us for 32 requests of 1000 to 6000 rows, 8 heads).  4-bit
 // rows: a unit of 32 rows and 128 channels is about 1050 instructions of a warp, half of them logical operations or additions of
-// whole numbers at two cycles each, and 72 products at eight: 2.5 TB/s (84 us for 32 requests of 1000 to 8000 rows; 32 us of DRAM).
+// whole numbers at two cycles each, and 72 products at eight: 2.7 TB/s (78 us for 32 requests of 1000 to 8000 rows; 32 us of DRAM).
 #include "cache_mma.cuh"
 #include "tc_ptx.cuh"
 
@@ -170,10 +172,16 @@ __device__ __forceinline__ void st_row(__nv_bfloat16* p, const float (&x)[4]) {
 }
 
 // Counters in shared memory through which warps hand results to one another.
-__device__ __forceinline__ int add_count(int* p) {
-  int old;
-  asm volatile("atom.acq_rel.cta.shared::cta.add.s32 %0, [%1], 1;" : "=r"(old) : "r"(smem_addr(p)) : "memory");
-  return old;
+__device__ __forceinline__ void arrive(int* p, int n) {
+  asm volatile("red.release.cta.shared::cta.add.s32 [%0], %1;" ::"r"(smem_addr(p)), "r"(n) : "memory");
+}
+// Of n + (n << 8), all of the warps: marks them as taken, for one caller.
+__device__ __forceinline__ bool take_full(int* p) {
+  int x, old;
+  asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(x) : "r"(smem_addr(p)) : "memory");
+  if (x == 0 || (x & 255) != x >> 8) return false;
+  asm volatile("atom.acquire.cta.shared::cta.cas.b32 %0, [%1], %2, %3;" : "=r"(old) : "r"(smem_addr(p)), "r"(x), "r"(1 << 30) : "memory");
+  return old == x;
 }
 __device__ __forceinline__ void set_count(int* p, int n) {
   asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_addr(p)), "r"(n) : "memory");
@@ -209,8 +217,8 @@ struct RowsSmem {
   static constexpr size_t RING = (size_t)W * ST * C::STAGE, WEIGHTS = (size_t)W * (HEADS * PK + (C::F32 ? HEADS * D : 0)) * 4,
                           CURSORS = (size_t)W * sizeof(Cursor<T, D, GROUP>), RESULTS = (size_t)W * RESULT * 4;
   // places for all warps' results of a pair: two if they fit
-  static constexpr int PLACES = RING + WEIGHTS + CURSORS + 2 * RESULTS + 16 <= 227 * 1024 ? 2 : 1;
-  static constexpr size_t BYTES = RING + WEIGHTS + CURSORS + PLACES * RESULTS + 16;
+  static constexpr int PLACES = RING + WEIGHTS + CURSORS + 2 * RESULTS + 48 <= 227 * 1024 ? 2 : 1;
+  static constexpr size_t BYTES = RING + WEIGHTS + CURSORS + PLACES * RESULTS + 48;
   static_assert(C::STAGE >= RESULT * 4 && WEIGHTS % 16 == 0 && CURSORS % 16 == 0, "a warp's results fit a stage; 16-byte pieces");
 };
 
@@ -708,6 +716,11 @@ __device__ __forceinline__ void int4_unit32(Running32<D, HEADS>& R, const float 
 }
 
 // ------------------------------------------------------------------ the kernel
+// Results of the warps that had units of a pair: warp w's at of + w * RESULT.
+struct Entry {
+  const float* of;
+  int r, g, flags;                               // flags: how many warps, << 8 the first, << 16 the whole pair, << 17 it begins here
+};
 template <typename T, int D, int GROUP, bool kTwo, int W, int ST>
 __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   using C = RowsCfg<T, D, GROUP>;
@@ -718,7 +731,8 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   float* weights = (float*)(smem_raw + M::RING);
   Cursor<T, D, GROUP>* cursors = (Cursor<T, D, GROUP>*)(smem_raw + M::RING + M::WEIGHTS);
   float* results = (float*)(smem_raw + M::RING + M::WEIGHTS + M::CURSORS);       // [place][warp][RESULT]
-  int *arrived = (int*)(results + M::PLACES * W * M::RESULT), *merged = arrived + 2;     // per place
+  int4* entries = (int4*)(results + M::PLACES * W * M::RESULT);                 // per place: r, g, flags of an Entry
+  int *arrived = (int*)(entries + 2), *merged = arrived + 2;                     // per place: how many warps and, << 8, of how many
   const CacheParams& c = P.c;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = c.Hq / c.Hkv;
   if (threadIdx.x < 4) arrived[threadIdx.x] = 0;
@@ -776,7 +790,92 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
   const int n = lane >> 2, j = lane & 3, head = kTwo ? n & 3 : n;
   float* sp = weights + warp * HEADS * PK;
   float* qs = weights + W * HEADS * PK + warp * HEADS * D;                       // (fp32: queries)
+  // Puts the results of a pair's warps together, in their order.
+  auto merge = [&](const Entry& e) {
+    const float* of = e.of;
+    const bool whole = e.flags >> 16 & 1;
+    const int64_t share = (int64_t)blockIdx.x * 2 + (e.flags >> 17 & 1), at = (int64_t)e.r * c.Hq + e.g * G;
+    // a lane per warp and head: the warp's factor to the head's largest reference, that and the head's sum; they go where the weights
+    // were.  (Short loops: code that runs once per pair is not in the instruction cache.)
+    constexpr int PW = W <= 4 ? 4 : W <= 8 ? 8 : 16, HP = 32 / PW;
+    static_assert(HEADS * (PW + 2) <= HEADS * PK, "room");
+    float2* of_head = reinterpret_cast<float2*>(sp + HEADS * PW);
+    const int w0 = lane % PW;
+    const bool has = w0 < W && (w0 + W - (e.flags >> 8 & 255)) % W < (e.flags & 255);
+    const uint32_t live = __ballot_sync(0xffffffffu, has);
+#pragma unroll 1
+    for (int h = lane / PW; h < (HEADS > HP ? HEADS : HP); h += HP) {            // (whole warps)
+      const float2 t = has && h < G ? *reinterpret_cast<const float2*>(of + w0 * M::RESULT + M::STATS + 2 * h) : make_float2(kNoWeight, 0.f);
+      float top = t.x;
+#pragma unroll
+      for (int y = PW / 2; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+      const float f = ex2a(t.x - top);
+      float sum = t.y * f;
+#pragma unroll
+      for (int y = PW / 2; y > 0; y >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
+      if (h < HEADS) {
+        sp[h * PW + w0] = f;
+        if (w0 == 0) of_head[h] = make_float2(top, sum);
+      }
+    }
+    __syncwarp();
+    constexpr int CL = D / 32;                       // channels of a lane
+#pragma unroll 1
+    for (int h = 0; h < G; ++h) {
+      // (all loads first, so that they are on their way together)
+      float x[W][CL], z[W], f[PW], acc[CL] = {};
+#pragma unroll
+      for (int w = 0; w < W; w += 4) {
+        const float4 y = *reinterpret_cast<const float4*>(sp + h * PW + w);
+        f[w] = y.x; f[w + 1] = y.y; f[w + 2] = y.z; f[w + 3] = y.w;
+      }
+      const float2 total = of_head[h];
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+#pragma unroll
+        for (int i = 0; i < CL; ++i) x[w][i] = 0.f;
+        z[w] = 0.f;
+        if (live >> w & 1) {
+          ld_floats(x[w], of + w * M::RESULT + h * D + lane * CL);
+          if constexpr (C::INT4 && !C::F32) z[w] = of[w * M::RESULT + M::ZEROS + h * NG + lane * CL / GROUP];
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < CL; ++i) acc[i] = fmaf(x[w][i] + z[w], f[w], acc[i]);
+      if (whole) {
+        const float inv = 1.f / total.y;
+#pragma unroll
+        for (int i = 0; i < CL; ++i) acc[i] *= inv;
+        st_row((T*)c.out + (at + h) * D + lane * CL, acc);
+        if (c.lse && lane == 0) c.lse[at + h] = (total.x + log2f(total.y)) * kLn2;
+      } else {
+        st_row(P.shares + (share * G + h) * D + lane * CL, acc);
+        if (lane == 0) *reinterpret_cast<float2*>(P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2) = total;
+      }
+    }
+    __syncwarp();
+  };
+  // The results in a place, if all are there and nobody else has taken them.
+  auto take = [&](int place, Entry& e) {
+    int got = 0;
+    if (lane == 0) got = take_full(arrived + place);
+    if (!__shfl_sync(0xffffffffu, got, 0)) return false;
+    const int4 x = entries[place];
+    e.r = x.x; e.g = x.y; e.flags = x.z;
+    e.of = results + place * W * M::RESULT;
+    return true;
+  };
+  auto leave = [&](int place) {
+    if (lane == 0) {
+      arrived[place] = 0;
+      set_count(merged + place, merged[place] + 1);
+    }
+  };
   int k = 0, shared = 0;                             // this warp's units so far; pairs so far that several warps had
+  Entry own;
+  bool alone = false, late = false;                  // (alone: `own` is to be put together)
   for (int u = u0, end; u < u1; u = end) {           // pair by pair
     work.seek(c, P.n_req, u);
     end = min(work.start + work.units, u1);
@@ -785,13 +884,23 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     const int parts = min(W, end - u), head_warp = (u - u0) % W;
     const int place = shared % M::PLACES, before = shared / M::PLACES;
     if (parts > 1) ++shared;
-    if ((warp + W - head_warp) % W >= parts) continue;
     // Where its results go: by itself a warp takes the one stage of its ring that holds no unit to come, otherwise its part of a
-    // place whose last pair has been put together.
+    // place.  The first warp that finds the place's last pair complete puts that together: it is the one with the most time.
+#pragma unroll 1
+    for (;;) {
+      Entry e;
+      const bool taken = !alone && parts > 1 && before > 0 && take(place, e);
+      if (!alone && !taken) break;
+      if (alone) e = own;
+      merge(e);
+      if (taken) leave(place);
+      alone = false;
+    }
+    if ((warp + W - head_warp) % W >= parts) continue;
     float* mine;
     auto open_place = [&]() {
       mine = parts == 1 ? (float*)(my_ring + (size_t)((k + ST - 1) % ST) * C::STAGE) : results + (place * W + warp) * M::RESULT;
-      return parts == 1 || wait_count(merged + place, before, P.status, P.limit);
+      return parts == 1 || before == 0 || wait_count(merged + place, before, P.status, P.limit);
     };
     if constexpr (C::F32) {
       Running32<D, HEADS> R;
@@ -828,7 +937,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           dense32_unit<D, HEADS, C::TAIL>(R, qs, st, st + C::TAIL * D * 4, valid, c.scale2, sp, lane);
         }
       }
-      if (!open_place()) break;
+      if ((late = !open_place())) break;
 #pragma unroll
       for (int h = 0; h < HEADS; ++h) {
 #pragma unroll
@@ -885,7 +994,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           }
         }
       }
-      if (!open_place()) break;
+      if ((late = !open_place())) break;
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) {
         R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
@@ -918,88 +1027,31 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
         }
       }
     }
-    // --- the warp that comes last puts the results together, in their order; nobody waits for it
+    own.r = work.r; own.g = work.g;
+    own.flags = parts | head_warp << 8 | (work.start >= u0 && work.start + work.units <= u1) << 16 | (work.start >= u0) << 17;
+    own.of = mine - warp * M::RESULT;
     __syncwarp();
-    if (parts > 1) {
-      int last = 0;
-      if (lane == 0) last = add_count(arrived + place) == parts - 1;
-      if (!__shfl_sync(0xffffffffu, last, 0)) continue;
-    }
-    const float* of = parts == 1 ? mine - warp * M::RESULT : results + place * W * M::RESULT;      // warp w's at w * RESULT
-    const bool whole = work.start >= u0 && work.start + work.units <= u1;
-    const int64_t share = (int64_t)blockIdx.x * 2 + (work.start >= u0 ? 1 : 0), at = (int64_t)work.r * c.Hq + work.g * G;
-    // a lane per warp and head: the warp's factor to the head's largest reference, that and the head's sum; they go where the weights
-    // were.  (Short loops: code that runs once per pair is not in the instruction cache.)
-    constexpr int PW = W <= 4 ? 4 : W <= 8 ? 8 : 16, HP = 32 / PW;
-    static_assert(HEADS * (PW + 2) <= HEADS * PK, "room");
-    float2* of_head = reinterpret_cast<float2*>(sp + HEADS * PW);
-    const int w0 = lane % PW;
-    const bool has = w0 < W && (w0 + W - head_warp) % W < parts;
-    const uint32_t live = __ballot_sync(0xffffffffu, has);
-#pragma unroll 1
-    for (int h = lane / PW; h < (HEADS > HP ? HEADS : HP); h += HP) {            // (whole warps)
-      const float2 t = has && h < G ? *reinterpret_cast<const float2*>(of + w0 * M::RESULT + M::STATS + 2 * h) : make_float2(kNoWeight, 0.f);
-      float top = t.x;
-#pragma unroll
-      for (int y = PW / 2; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-      const float f = ex2a(t.x - top);
-      float sum = t.y * f;
-#pragma unroll
-      for (int y = PW / 2; y > 0; y >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
-      if (h < HEADS) {
-        sp[h * PW + w0] = f;
-        if (w0 == 0) of_head[h] = make_float2(top, sum);
-      }
-    }
-    __syncwarp();
-    constexpr int CL = D / 32;                       // channels of a lane
-#pragma unroll 1
-    for (int h = 0; h < G; ++h) {
-      // (all loads first, so that they are on their way together)
-      float x[W][CL], z[W], f[PW], acc[CL] = {};
-#pragma unroll
-      for (int w = 0; w < W; w += 4) {
-        const float4 y = *reinterpret_cast<const float4*>(sp + h * PW + w);
-        f[w] = y.x; f[w + 1] = y.y; f[w + 2] = y.z; f[w + 3] = y.w;
-      }
-      const float2 total = of_head[h];
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-#pragma unroll
-        for (int e = 0; e < CL; ++e) x[w][e] = 0.f;
-        z[w] = 0.f;
-        if (live >> w & 1) {
-          ld_floats(x[w], of + w * M::RESULT + h * D + lane * CL);
-          if constexpr (C::INT4 && !C::F32) z[w] = of[w * M::RESULT + M::ZEROS + h * NG + lane * CL / GROUP];
-        }
-      }
-#pragma unroll
-      for (int w = 0; w < W; ++w)
-#pragma unroll
-        for (int e = 0; e < CL; ++e) acc[e] = fmaf(x[w][e] + z[w], f[w], acc[e]);
-      if (whole) {
-        const float inv = 1.f / total.y;
-#pragma unroll
-        for (int e = 0; e < CL; ++e) acc[e] *= inv;
-        st_row((T*)c.out + (at + h) * D + lane * CL, acc);
-        if (c.lse && lane == 0) c.lse[at + h] = (total.x + log2f(total.y)) * kLn2;
-      } else {
-        st_row(P.shares + (share * G + h) * D + lane * CL, acc);
-        if (lane == 0) *reinterpret_cast<float2*>(P.shares + share_stats(gridDim.x, G, D) + (share * G + h) * 2) = total;
-      }
-    }
-    __syncwarp();
-    if (parts > 1 && lane == 0) {
-      arrived[place] = 0;
-      set_count(merged + place, before + 1);
+    alone = parts == 1;
+    if (!alone && lane == 0) {
+      if (warp == head_warp) entries[place] = make_int4(own.r, own.g, own.flags, 0);
+      arrive(arrived + place, warp == head_warp ? 1 + (parts << 8) : 1);
     }
   }
   copy_wait<0>();
+  // What is left.  (Every warp looks at a place at least once after its last contribution to it, here or above: no result stays.)
+#pragma unroll 1
+  for (int place = -1; place < min(M::PLACES, shared) && !late; ++place) {
+    Entry e = own;
+    if (place < 0 ? !alone : !take(place, e)) continue;
+    merge(e);
+    if (place >= 0) leave(place);
+  }
 }
 
 // Pairs that lie in several CTAs, from the shares these left: a CTA per pair where there are fewer pairs than CTAs, else one per
-// boundary, for the pair that goes on from CTA blockIdx.x to the next, if it began in that CTA.  A thread sums four channels of every `parts`-th share; what it reads first is on its way while the shares'
-// references are compared.  And the outputs of requests without any row.
+// boundary, for the pair that goes on from CTA blockIdx.x to the next, if it began in that CTA.  A thread sums four channels of
+// every `parts`-th share; what it reads first is on its way while the shares' references are compared.  And the outputs of
+// requests without any row.
 constexpr int M_THREADS = 512, M_AHEAD = 6;
 template <typename T, int D, int GROUP>
 __global__ void __launch_bounds__(M_THREADS) merge_shares(const RowsParams P, int ctas, bool by_pair) {
@@ -1124,8 +1176,9 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
 template <typename T, int D, int GROUP>
 cudaError_t run_rows(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
   // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, fp32 rows 3 x 2 of up to
-  // 32 KB, 4-bit rows of 128 channels 8 x 3 of 5 to 6 KB (12 x 2: 32 requests as fast, one request of 4096 rows 13.4 us instead of
-  // 12.8; 16 x 2, with 128 registers a thread, 8 % slower), of 64 channels 12 x 2 (8 x 3: 6 % slower).
+  // 32 KB, 4-bit rows of 128 channels 8 x 3 of 5 to 6 KB (12 x 2: one request of 144000 rows 5 % faster, 32 ragged ones as fast,
+  // one of 4096 rows and 256 of 560 4 % and eight heads on one 14 % slower; 16 x 2, with 128 registers a thread, 8 % slower), of 64
+  // channels 12 x 2 (8 x 3: 6 % slower).
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int W = !GROUP ? (F32 ? 3 : 4) : F32 || D == 128 ? 8 : 12, ST = (GROUP ? D == 128 && !F32 : !F32) ? 3 : 2;
   return P.c.Hq / P.c.Hkv <= 4 ? run_units<T, D, GROUP, true, W, ST>(ctx, P, st) : run_units<T, D, GROUP, false, W, ST>(ctx, P, st);

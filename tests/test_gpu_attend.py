@@ -718,3 +718,18 @@ def test_calls_among_copies_and_other_streams_in_a_graph(group):
             t.fill_(7)
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("group", [0, 32])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 1, 64), (16, 16, 64)])
+def test_cache_short_ragged_requests_repeat_bit_for_bit(hq, hkv, d, group):
+    """Many pairs end inside a CTA, of one unit or of a few more than it has warps: whichever warp puts results together, and when."""
+    rng = np.random.default_rng(hq + d + group)
+    lens = tuple(int(n) for n in rng.choice([0, 1, 20, 33, 64, 65, 130, 260, 300, 390, 600], size=250))
+    cake = context(hq, hkv, d, BF16, layers=1)
+    x = cached(hq, hkv, d, BF16, lens, group=group, layers=1, layer=0, tail=(20, rng.integers(0, 21, size=250)))
+    out, lse = check_cached(cake, x, BF16)
+    for _ in range(40):
+        again, lse2 = run_cached(cake, x)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+    assert cake.status() == 0
