@@ -343,7 +343,7 @@ int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t
  *   lse_window  optional [n_req][H_q][S_w] fp32: the same of the last S_w rows of every request, as
  *         cake_score_layer takes it (its scoring is then one pass instead of two)
  * What lies behind a row (later tokens, other requests) has no influence on it, not even an infinity or
- * a NaN there.  (fp32 is computed in three bf16 terms per number, exact to the last bit or two of a finite
+ * a NaN there; a logit of -inf weighs nothing.  (fp32 is computed in three bf16 terms per number, exact to the last bit or two of a finite
  * one; an infinity that a row does see may make it a NaN.) */
 int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
                            const void* k, const void* v, void* out, int64_t out_head_stride,
