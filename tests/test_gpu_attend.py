@@ -733,3 +733,30 @@ def test_cache_short_ragged_requests_repeat_bit_for_bit(hq, hkv, d, group):
         again, lse2 = run_cached(cake, x)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
     assert cake.status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_calls_on_two_streams_at_once(d):
+    """Prompts of one context beside prompts and caches of another, on streams of their own: the same as one by one."""
+    lens, group = (1500, 260), 32
+    work = []
+    for dtype in (BF16, FP32):
+        x = cached(8, 2, d, dtype, (900, 130, 33), group=group, tail=(9, np.array([9, 0, 4])), seed=8)
+        work.append((context(8, 2, d, dtype, lens, layers=2), prompt(8, 2, d, dtype, lens, seed=d), x))
+
+    def step(cake, qkv, x):
+        out, lse = cake.attend_prompt(*qkv)
+        return out, lse, cake.accumulate_attention(qkv[0], qkv[1], lse), *run_cached(cake, x)
+
+    want = [step(*w) for w in work]
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s, w in zip(streams, work):
+            with torch.cuda.stream(s):
+                got.append(step(*w))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
+    assert all(cake.status() == 0 for cake, *_ in work)
