@@ -359,7 +359,7 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
     if (ok && n) {
       tc_fence_after();
       const int i = row0 + t * TILE + row;       // the row in its request
-      if (ref == kNoWeight) sum = 0.f;           // (the polynomial does not go below 2^-127)
+      // (logits of -inf alone: a sum of zero, no output and an lse of -inf; with a NaN among them the sum is one, and so is the lse)
       const float inv = sum == 0.f ? CUDART_NAN_F : 1.f / sum;
       const bool live = i < N;
       __nv_bfloat16* dst = P.out + h * P.os.head + (cu + i) * P.os.token;

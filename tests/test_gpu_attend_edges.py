@@ -1,0 +1,33 @@
+"""Attention over prompts and caches where it can go wrong: values that are no numbers, that overflow or are huge, sums that have a
+closed form, arguments that do not fit, waits that run out."""
+import pytest
+import torch
+
+from test_gpu_attend import BF16, FP32, context, prompt
+
+pytestmark = pytest.mark.gpu
+DTYPES = pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
+
+
+@DTYPES
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_logits_that_are_no_numbers(dtype, d):
+    """A row with a NaN among its logits has a log-sum-exp of NaN, not the -inf of a row without weight: a query that is NaN, and a
+    first key that is (then row 0 sees nothing else, and the maximum of no logit of the first tile can be taken for a number)."""
+    lens, sw = (300, 40), 16
+    cake = context(4, 2, d, dtype, lens, window=sw)
+    q, k, v = prompt(4, 2, d, dtype, lens, seed=6)
+    good, good_lse = cake.attend_prompt(q, k, v)
+    bad = torch.zeros(4, 340, dtype=torch.bool, device="cuda")
+    q[:2, [0, 5, 200, 299], 3] = float("nan")
+    bad[:2, [0, 5, 200, 299]] = True
+    k[1, 300, 1] = float("nan")                       # the second request's first key, for heads 2 and 3
+    bad[2:, 300:] = True
+    q[1, 310] = float("nan")                          # every channel
+    bad[1, 310] = True
+    lw = torch.full((2, 4, sw), 7.0, device="cuda")
+    out, lse = cake.attend_prompt(q, k, v, lse_window=lw)
+    assert torch.equal(torch.isnan(lse), bad) and torch.isnan(out[bad]).all()
+    assert torch.equal(lse[~bad], good_lse[~bad]) and torch.equal(out[~bad], good[~bad])
+    want = torch.stack([lse[:, a - sw:a] for a in (300, 340)])
+    assert torch.equal(torch.isnan(lw), torch.isnan(want)) and torch.equal(lw.nan_to_num(1.0), want.nan_to_num(1.0))
