@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
       const float top = fmaxf(m0, m1) * P.scale2;
       // The reference follows a maximum that is more than 2^kRefSlack above it.  (A factor is read before the logits of three
       // tiles on are issued, so that a ring of four is enough.)
-      const float to = j == 0 || top > ref + kRefSlack ? top : ref, f = j == 0 || to == ref ? 1.f : ex2(ref - to);
+      const float to = j == 0 ? fmaxf(top, kNoWeight) : top > ref + kRefSlack ? top : ref, f = j == 0 || to == ref ? 1.f : ex2(ref - to);
       ref = to;
       factors[(j % P_FACTORS) * TILE + row] = f;
       // weights, their sum, and their three planes

@@ -3,7 +3,8 @@ closed form, arguments that do not fit, waits that run out."""
 import pytest
 import torch
 
-from test_gpu_attend import BF16, FP32, context, prompt
+from oracle import cake_oracle as O
+from test_gpu_attend import BF16, FP32, check_out, context, f64, prompt, weight_error
 
 pytestmark = pytest.mark.gpu
 DTYPES = pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
@@ -31,3 +32,21 @@ def test_prompt_logits_that_are_no_numbers(dtype, d):
     assert torch.equal(lse[~bad], good_lse[~bad]) and torch.equal(out[~bad], good[~bad])
     want = torch.stack([lse[:, a - sw:a] for a in (300, 340)])
     assert torch.equal(torch.isnan(lw), torch.isnan(want)) and torch.equal(lw.nan_to_num(1.0), want.nan_to_num(1.0))
+
+
+@DTYPES
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [1, 63, 64, 65, 130, 256])
+def test_prompt_finite_inputs_whose_logits_overflow(dtype, d, bad):
+    """Finite queries and keys with logits of -inf, also where the first tiles of a row have no other: they weigh nothing."""
+    n = 300
+    cake = context(2, 1, d, dtype, (n,))
+    q, k, v = prompt(2, 1, d, dtype, (n,), seed=4)
+    q[:, :, 0] = 2.0 ** 66
+    k[:, :, 0] = 0
+    k[:, :bad, 0] = -(2.0 ** 66)
+    out, lse = cake.attend_prompt(q, k, v)
+    assert torch.isnan(out[:, :bad]).all() and (lse[:, :bad] == float("-inf")).all()
+    qn, kn, vn = f64(q[:, bad:]), f64(k[:, bad:]), f64(v[:, bad:])
+    qn[:, :, 0] = 0                                   # (times a key's zero)
+    check_out(f64(out[:, bad:]), f64(lse[:, bad:]), O.prompt_attention(qn, kn, vn), weight_error(qn, kn, d), n, dtype)
