@@ -398,7 +398,7 @@ class Cake:
                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
                      ) -> Tuple[torch.Tensor, torch.Tensor]:
         """Attention of one new token per request, q [n_req][H_q][d], over one layer of the packed cache that compact or
-        decode_begin returned, and over the first tail_len[r] rows of k_tail, v_tail [n_req][H_kv][capacity][d]:
+        decode_begin returned (k_cache, v_cache of the same [rows][d]), and over the first tail_len[r] rows of k_tail, v_tail [n_req][H_kv][capacity][d]:
         (out, lse [n_req][H_q]).  Does not depend on the context's current batch."""
         c = self.cfg
         rc, out, lse = _fast.attend_cache(self._a, self._fp32, layer, c.n_layers, c.n_q_heads, c.n_kv_heads, c.head_dim, q,

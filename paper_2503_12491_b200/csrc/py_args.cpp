@@ -491,7 +491,7 @@ PyObject* attend_cached(PyObject* const* a, bool int4) {
     const at::Tensor ws = at::empty({bytes}, q.options().dtype(u8));
     int32_t rc;
     if (!int4) {
-      const at::Tensor &k = tensor(a[14], "k_cache", e, {-1, d}), &v = tensor(a[15], "v_cache", e, {-1, d});
+      const at::Tensor &k = tensor(a[14], "k_cache", e, {-1, d}), &v = tensor(a[15], "v_cache", e, {k.size(0), d});
       rc = released([&](void* st) {
         return lib.attend_cache(c, (int32_t)R, (int32_t)layer, q.data_ptr(), rows_of(k, ws), rows_of(v, ws), off, t.k, t.v, t.len, t.cap,
                                 out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes, st);

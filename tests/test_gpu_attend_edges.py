@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import cake_oracle as O
-from test_gpu_attend import BF16, FP32, check_out, context, f64, prompt, weight_error
+from test_gpu_attend import BF16, FP32, cached, check_out, context, f64, prompt, run_cached, weight_error
 
 pytestmark = pytest.mark.gpu
 DTYPES = pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
@@ -50,3 +50,16 @@ def test_prompt_finite_inputs_whose_logits_overflow(dtype, d, bad):
     qn, kn, vn = f64(q[:, bad:]), f64(k[:, bad:]), f64(v[:, bad:])
     qn[:, :, 0] = 0                                   # (times a key's zero)
     check_out(f64(out[:, bad:]), f64(lse[:, bad:]), O.prompt_attention(qn, kn, vn), weight_error(qn, kn, d), n, dtype)
+
+
+# ------------------------------------------------------------------ arguments
+@DTYPES
+def test_keys_and_values_of_a_cache_have_the_same_rows(dtype):
+    """The offsets are those of both: values of another layer or an older compaction, with fewer rows, would be read past their end."""
+    x = cached(4, 2, 64, dtype, (40, 3))
+    cake = context(4, 2, 64, dtype, layers=2)
+    want = run_cached(cake, x)
+    for k, v in [(x["k"], x["v"][:-1]), (x["k"], x["v"][:5]), (x["k"][:-1], x["v"]), (x["k"], x["v"][:0])]:
+        with pytest.raises(ValueError, match="v_cache: expected shape"):
+            cake.attend_cache(1, x["q"], k, v, x["off"])
+    assert all(torch.equal(a, b) for a, b in zip(run_cached(cake, x), want))
