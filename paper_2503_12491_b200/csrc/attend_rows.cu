@@ -863,6 +863,7 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
     int got = 0;
     if (lane == 0) got = take_full(arrived + place);
     if (!__shfl_sync(0xffffffffu, got, 0)) return false;
+    __syncwarp();                                    // (a shuffle orders no memory: what lane 0 has acquired, the others read below)
     const int4 x = entries[place];
     e.r = x.x; e.g = x.y; e.flags = x.z;
     e.of = results + place * W * M::RESULT;

@@ -1,10 +1,11 @@
 """Attention over prompts and caches where it can go wrong: values that are no numbers, that overflow or are huge, sums that have a
 closed form, arguments that do not fit, waits that run out."""
+import numpy as np
 import pytest
 import torch
 
 from oracle import cake_oracle as O
-from test_gpu_attend import BF16, FP32, cached, check_out, context, f64, prompt, run_cached, weight_error
+from test_gpu_attend import BF16, FP32, cached, check_cached, check_out, context, f64, prompt, run_cached, weight_error
 
 pytestmark = pytest.mark.gpu
 DTYPES = pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
@@ -63,3 +64,19 @@ def test_keys_and_values_of_a_cache_have_the_same_rows(dtype):
         with pytest.raises(ValueError, match="v_cache: expected shape"):
             cake.attend_cache(1, x["q"], k, v, x["off"])
     assert all(torch.equal(a, b) for a, b in zip(run_cached(cake, x), want))
+
+
+# ------------------------------------------------------------------ results handed from warp to warp
+@pytest.mark.parametrize("group", [0, 32, 64])
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (8, 1)])
+def test_short_ragged_fp32_requests_repeat_bit_for_bit(hq, hkv, group):
+    """Most pairs end inside a CTA, where a warp puts together what the others left: always the same, and right."""
+    rng = np.random.default_rng(hq + group)
+    lens = tuple(int(n) for n in rng.choice([0, 1, 20, 33, 64, 65, 130, 260, 300, 390, 600], size=200))
+    cake = context(hq, hkv, 64, FP32, layers=1)
+    x = cached(hq, hkv, 64, FP32, lens, group=group, layers=1, layer=0, tail=(20, rng.integers(0, 21, size=200)))
+    out, lse = check_cached(cake, x, FP32)
+    for _ in range(40):
+        again, lse2 = run_cached(cake, x)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+    assert cake.status() == 0
