@@ -233,9 +233,9 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
       issued = i + 1;
     }
     // do not leave the CTA while a copy may still be writing its shared memory
-    mbar_wait(S.q_full, 0, P.status, P.limit);
+    mbar_drain(S.q_full, 0, P.status);
     for (int i = max(0, issued - C::STAGES); i < issued; ++i)
-      mbar_wait(full_of(i), diag_of(i) < 0 ? phase_of(i) : 0u, P.status, P.limit);
+      mbar_drain(full_of(i), diag_of(i) < 0 ? phase_of(i) : 0u, P.status);
   } else if (warp == W_MMA) {
     const uint32_t id_s = instr_desc(TILE, TILE), id_o = instr_desc(TILE, D) | (1u << 16);   // B of the second: N along the row
     const uint32_t q_lo = (smem_u32(S.q) & 0x3FFFFu) >> 4, kv_lo = (smem_u32(S.kv) & 0x3FFFFu) >> 4;
@@ -303,10 +303,9 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
         umma_commit(&S.kv_empty[stage_of(ki)]);
       }
     }
-    if (!ok) {                                   // what was issued ends before tensor and shared memory are given back
-      umma_commit(S.drained);
-      mbar_wait(S.drained, 0, P.status, P.limit);
-    }
+    // what was issued ends before tensor and shared memory are given back, whether the others have waited for it or not
+    umma_commit(S.drained);
+    mbar_drain(S.drained, 0, P.status);
   } else if (warp >= W_SCAN) {
     // the value tiles on the diagonals: j = n_a - 1 and n_b - 1
     for (int t = 0; t < (n_b ? 2 : 1); ++t) {
@@ -539,9 +538,9 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
       if (q0 >= N) { q0 = key0; ++h; }
     }
     // do not leave the CTA while a copy may still be writing its shared memory
-    mbar_wait(S.k_full, 0, P.status, P.limit);
+    mbar_drain(S.k_full, 0, P.status);
     for (int t = max(0, issued - A_STAGES); t < issued; ++t)
-      mbar_wait(&S.q_full[t % A_STAGES], (uint32_t)(t / A_STAGES) & 1u, P.status, P.limit);
+      mbar_drain(&S.q_full[t % A_STAGES], (uint32_t)(t / A_STAGES) & 1u, P.status);
   } else if (warp == A_MMA) {
     const uint32_t id = instr_desc(TILE, TILE);
     const uint32_t a = (smem_u32(S.k) & 0x3FFFFu) >> 4, q_lo = (smem_u32(S.q) & 0x3FFFFu) >> 4;
@@ -570,7 +569,7 @@ accumulate_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
       last = t;
     }
     // what was issued ends before tensor and shared memory are given back
-    if (last >= 0) mbar_wait(&S.acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status, P.limit);
+    if (last >= 0) mbar_drain(&S.acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status);
   } else if (warp == A_LSE) {
     // -lse * log2(e) of the queries of every tile, three tiles ahead in registers
     constexpr int AHEAD = 3;

@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(A_THREADS, 1) accumulate_tc32(const __grid_con
       last = t;
     }
     // what was issued ends before tensor and shared memory are given back
-    if (last >= 0) mbar_wait(&acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status, P.limit);
+    if (last >= 0) mbar_drain(&acc_full[last % A_BUFS], (uint32_t)(last / A_BUFS) & 1u, P.status);
   } else if (warp == A_LSE) {
     // -lse * log2(e) of the queries of every tile, three tiles ahead in registers
     constexpr int AHEAD = 3;
@@ -393,9 +393,12 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
       umma_commit(o_full);
       done = j + 1;
     }
-    if (!ok) {                                   // what was issued ends before tensor and shared memory are given back
+    // what was issued ends before tensor and shared memory are given back, whether the others have waited for it or not
+    // (one phase after the other: a parity does not tell a phase from the next but one)
+    if (done > 0) mbar_drain(o_full, (uint32_t)(done - 1) & 1u, P.status);
+    if (!ok) {
       umma_commit(o_full);
-      mbar_wait(o_full, (uint32_t)done & 1u, P.status, P.limit);
+      mbar_drain(o_full, (uint32_t)done & 1u, P.status);
     }
   } else if (warp >= P_CONV) {
     const int t256 = threadIdx.x - P_CONV * 32, c0 = ((warp - P_CONV) >> 2) * DH;

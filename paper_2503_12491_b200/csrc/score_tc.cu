@@ -394,9 +394,9 @@ score_fused_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       // do not leave the CTA while a bulk copy may still be writing its shared memory
       const uint32_t issued = t;
       for (uint32_t u = issued > STAGES ? issued - STAGES : 0; u < issued; ++u)
-        mbar_wait(&S.full[u % STAGES], (u / STAGES) & 1, P.status, P.spin_limit);
+        mbar_drain(&S.full[u % STAGES], (u / STAGES) & 1, P.status);
       for (uint32_t u = qn > 2 ? qn - 2 : 0; u < qn; ++u)
-        mbar_wait(&S.q_full[u & 1], (u >> 1) & 1, P.status, P.spin_limit);
+        mbar_drain(&S.q_full[u & 1], (u >> 1) & 1, P.status);
     }
   } else if (warp == WARP_MMA) {
     // ------------------------------------------------ MMA issuer (converged warp, elected lane issues)
@@ -468,6 +468,8 @@ score_fused_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
           ++kbm;
         }
       }
+      // the last tile's products, and with them all before, end before the CTA does
+      if (t > 0) mbar_drain(&S.acc_full[(t - 1) % NBUF], ((t - 1) / NBUF) & 1, P.status);
     }
   } else if (warp == WARP_MERGE) {
     // ------------------------------------------------ row merger

@@ -68,6 +68,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int32_
   }
   return true;
 }
+// Until copies and products of this CTA that are on their way have ended, before it gives back its shared and tensor memory.  They
+// end by themselves, so the limit that a caller has set for the other waits, however short, is not theirs.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity, int32_t* status) { mbar_wait(bar, parity, status, kSpinLimit); }
 // 3-D tiled TMA load with an L2 eviction-priority hint: a whole key tile (both 64-element slabs)
 // in one copy.
 __device__ __forceinline__ void tma_load_3d_hint(void* dst, const CUtensorMap* map, uint64_t* bar,

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle import cake_oracle as O
+from paper_2503_12491_b200.binding import CAKE_ERR_TIMEOUT
 from test_gpu_attend import BF16, FP32, cached, check_cached, check_out, context, f64, prompt, run_cached, weight_error
 
 pytestmark = pytest.mark.gpu
@@ -80,3 +81,38 @@ def test_short_ragged_fp32_requests_repeat_bit_for_bit(hq, hkv, group):
         again, lse2 = run_cached(cake, x)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
     assert cake.status() == 0
+
+
+# ------------------------------------------------------------------ waits that run out
+@DTYPES
+@pytest.mark.parametrize("d", [64, 128])
+def test_waits_that_run_out_leave_the_context_usable(d, dtype):
+    """A limit of one cycle.  (A wait on an mbarrier looks twice and sleeps for microseconds in between, so that short ones may still
+    succeed: those of whole prompts in bf16 do not, nor those of warps for results of one another.)  Every kernel ends, after the
+    copies and products that it has on their way, whatever the limit; the status says so; a call that reports nothing is right; and
+    afterwards everything is as before."""
+    lens, rows = (3000, 100), (60,) * 300
+    cu = np.concatenate([[0], np.cumsum(lens)]).tolist()
+    cake = context(8, 2, d, dtype, lens, layers=2)
+    q, k, v = prompt(8, 2, d, dtype, lens)
+    caches = [cached(8, 2, d, dtype, rows, group=g) for g in (0, 32)]
+    lse = cake.attend_prompt(q, k, v)[1]
+    calls = [lambda: cake.attend_prompt(q, k, v), lambda: (cake.accumulate_attention(q, k, lse),),
+             lambda: run_cached(cake, caches[0]), lambda: run_cached(cake, caches[1])]
+    good = [f() for f in calls]
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip(a, b))
+    assert cake.status() == 0
+    for i, f in enumerate(calls):
+        ran_out = 0
+        for _ in range(5):
+            cake.begin(cu)
+            cake.set_wait_limit(1)
+            got = f()
+            cake.set_wait_limit(0)
+            status = cake.status()
+            assert status in (0, CAKE_ERR_TIMEOUT)
+            ran_out += status != 0
+            assert status != 0 or same(got, good[i])
+        assert ran_out or i == 1 or dtype == FP32
+        cake.begin(cu)
+        assert all(same(c(), w) for c, w in zip(calls, good)) and cake.status() == 0
