@@ -487,11 +487,12 @@ __global__ void __launch_bounds__(P_THREADS, 1) prompt_tc32(const __grid_constan
       const float to = j == 0 ? fmaxf(top, kNoWeight) : top > ref + kRefSlack ? top : ref, f = j == 0 || to == ref ? 1.f : ex2(ref - to);
       ref = to;
       factors[(j % P_FACTORS) * TILE + row] = f;
+      const float cf = coarse_factor(ref), sc = P.scale2 * cf, mr = -ref * cf;
       // weights, their sum, and their three planes
       float part[4] = {};
 #pragma unroll
       for (int c = 0; c < 64; ++c) {
-        s[c] = ex2(fmaf(s[c], P.scale2, -ref));
+        s[c] = ex2(fmaf(s[c], sc, mr));
         part[c & 3] += s[c];
       }
       sum = fmaf(sum, f, (part[0] + part[1]) + (part[2] + part[3]));
