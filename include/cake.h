@@ -327,8 +327,9 @@ int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t
  * These calls do not advance the context's batch: they may come at any point of it, on any stream, and
  * several times.  They allocate nothing, synchronise nothing, and a stream capture may record them.  A bounded wait
  * that runs out in one of their kernels shows in cake_status as CAKE_ERR_TIMEOUT, as elsewhere.
- * Tensors must start on 16-byte boundaries, and the context's device must be the current one, else
- * CAKE_ERR_ARG. */
+ * Queries, keys, values, outputs, 4-bit rows with their scales and zeros, and workspaces must start on 16-byte boundaries; what is
+ * held in whole numbers, log-sum-exps and accumulated weights on those of their elements.  The context's device must be the
+ * current one.  Else CAKE_ERR_ARG. */
 
 /* Causal attention over the prompts of the current batch (cake_begin), one layer:
  *   O_i = sum_{j <= i} softmax_j(q_i . k_j / sqrt(d)) v_j   inside each request,

@@ -69,6 +69,9 @@ struct Strided {
   int64_t head, token;
 };
 
+// A null pointer is aligned: whether it may be null is another check.
+inline bool aligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
 // Cached rows of one layer and the queries of one token per request.  group: channels (and rows) that share a scale in 4 bits,
 // 0 for rows of the context's type.
 struct CacheParams {

@@ -34,7 +34,7 @@ static constexpr int64_t kMaxHeadStride = (int64_t)1 << 38, kMaxTokenStride = (i
 // Rows that the kernels read and write in 16-byte pieces.
 static bool rows_ok(const cake_ctx* ctx, const void* p, int64_t head, int64_t token) {
   const int64_t es = ctx->cfg.dtype == CAKE_DTYPE_FP32 ? 4 : 2;
-  return ((uintptr_t)p & 15) == 0 && head >= 0 && token >= 0 && head < kMaxHeadStride && token < kMaxTokenStride &&
+  return aligned(p, 16) && head >= 0 && token >= 0 && head < kMaxHeadStride && token < kMaxTokenStride &&
          head * es % 16 == 0 && token * es % 16 == 0;
 }
 
@@ -62,6 +62,7 @@ int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, 
   if (!q || !k || !v || !out) return CAKE_ERR_ARG;
   if (!queries_ok(ctx, q, q_head_stride, q_token_stride) || !rows_ok(ctx, k, 0, 0) || !rows_ok(ctx, v, 0, 0) ||
       !rows_ok(ctx, out, out_head_stride, out_token_stride)) return CAKE_ERR_ARG;
+  if (!aligned(lse, 4) || !aligned(lse_window, 4)) return CAKE_ERR_ARG;
   // rows of the output that share memory would be written twice
   const int64_t heads = ctx->cfg.n_q_heads, tokens = ctx->total_tokens;
   const bool by_token = out_head_stride >= d && out_token_stride >= d && out_token_stride - d >= (heads - 1) * out_head_stride;
@@ -78,6 +79,7 @@ int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_s
   if (ok != CAKE_OK || ctx->n_req == 0) return ok;
   if (!q || !k || !lse || !out) return CAKE_ERR_ARG;
   if (!queries_ok(ctx, q, q_head_stride, q_token_stride) || !rows_ok(ctx, k, 0, 0)) return CAKE_ERR_ARG;
+  if (!aligned(lse, 4) || !aligned(out, 4)) return CAKE_ERR_ARG;
   const Strided qs = {q_head_stride, q_token_stride};
   return (ctx->cfg.dtype == CAKE_DTYPE_FP32 ? launch_accumulate_tc32 : launch_accumulate_tc)(ctx, q, qs, k, lse, out, (cudaStream_t)stream);
 }

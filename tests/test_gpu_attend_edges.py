@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import cake_oracle as O
-from paper_2503_12491_b200.binding import CAKE_ERR_TIMEOUT
+from paper_2503_12491_b200.binding import CAKE_ERR_ARG, CAKE_ERR_TIMEOUT
 from test_gpu_attend import BF16, FP32, U, cached, check_cached, check_out, context, f64, prompt, run_cached, weight_error
 
 pytestmark = pytest.mark.gpu
@@ -134,6 +134,58 @@ def test_keys_and_values_of_a_cache_have_the_same_rows(dtype):
         with pytest.raises(ValueError, match="v_cache: expected shape"):
             cake.attend_cache(1, x["q"], k, v, x["off"])
     assert all(torch.equal(a, b) for a, b in zip(run_cached(cake, x), want))
+
+
+@DTYPES
+def test_arguments_on_wrong_boundaries_are_refused(dtype):
+    """Log-sum-exps, accumulated weights and offsets lie on boundaries of their elements, at any of them; pointers off these are
+    refused before a launch."""
+    lens, sw = (40, 33), 4
+    cake = context(4, 2, 64, dtype, lens, window=sw, layers=2)
+    lib, h, p = cake.lib, cake._h, lambda t, off=0: t.data_ptr() + off
+    q, k, v = prompt(4, 2, 64, dtype, lens)
+    want, want_lse = cake.attend_prompt(q, k, v)
+    want_sum = cake.accumulate_attention(q, k, want_lse)
+    out, lse = torch.empty_like(q), torch.zeros(4 * 73 + 1, device="cuda")
+    lw, acc = torch.zeros(2 * 4 * sw + 1, device="cuda"), torch.zeros(2 * 73 + 1, device="cuda")
+    heads, tokens = 73 * 64, 64
+
+    def attend(lse_off, lw_off):
+        return lib.cake_attend_prompt(h, p(q), heads, tokens, p(k), p(v), p(out), heads, tokens, p(lse, lse_off), p(lw, lw_off), None)
+
+    def accumulate(lse_off, out_off):
+        return lib.cake_accumulate_attention(h, p(q), heads, tokens, p(k), p(lse, lse_off), p(acc, out_off), None)
+
+    assert [attend(2, 0), attend(1, 0), attend(0, 2), attend(0, 3), accumulate(2, 0), accumulate(0, 1)] == [CAKE_ERR_ARG] * 6
+    torch.cuda.synchronize()
+    assert attend(4, 4) == 0 and accumulate(4, 4) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse[1:].view(4, 73), want_lse) and torch.equal(acc[1:].view(2, 73), want_sum)
+    assert torch.equal(lw[1:].view(2, 4, sw), torch.stack([want_lse[:, a - sw:a] for a in (40, 73)]))
+
+    for group in (0, 32):
+        x = cached(4, 2, 64, dtype, (40, 3), group=group, tail=(4, np.array([1, 2])))
+        want, want_lse = run_cached(cake, x)
+        need = lib.cake_attend_workspace_bytes(h, 2)
+        ws, out = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(want)
+        lse, off = torch.zeros(9, device="cuda"), torch.cat([x["off"][:1], x["off"]])
+        tl = torch.cat([x["tail"]["tail_len"][:1], x["tail"]["tail_len"]])
+        c = x.get("cache")
+        koff = torch.cat([c["kgroup_offsets"][:1], c["kgroup_offsets"]]) if group else None
+
+        def call(o=8, t=4, l=4, g=8):
+            tail = (p(x["tail"]["k_tail"]), p(x["tail"]["v_tail"]), p(tl, t), 4, p(out), p(lse, l), p(ws), need, None)
+            if group:
+                return lib.cake_attend_int4(h, 2, 1, p(x["q"]), p(c["k_codes"]), p(c["k_scale"]), p(c["k_zero"]), p(c["v_codes"]),
+                                            p(c["v_scale"]), p(c["v_zero"]), group, p(off, o), p(koff, g), *tail)
+            return lib.cake_attend_cache(h, 2, 1, p(x["q"]), p(x["k"]), p(x["v"]), p(off, o), *tail)
+
+        assert [call(o=4), call(o=1), call(t=2), call(l=2), call(l=1)] == [CAKE_ERR_ARG] * 5
+        assert not group or call(g=4) == CAKE_ERR_ARG
+        torch.cuda.synchronize()
+        assert call() == 0
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse[1:].view(2, 4), want_lse)
 
 
 # ------------------------------------------------------------------ results handed from warp to warp
