@@ -425,16 +425,17 @@ prompt_tc(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUt
 //     D[key][query] = K Q^T  (tcgen05)  ->  sum over the queries of 2^(d * scale - lse)
 // A thread owns a key, so that its sum never leaves its registers; three groups of four warps take the query tiles in turn and
 // are added up at the end in a fixed order.  The queries' log-sum-exps of a tile come through shared memory, where all
-// threads of a warp read the same four at a time.  Where there are few tiles of keys, the heads of a group go to CTAs of their
-// own, a cluster, whose first adds up the others' sums (1000 tokens, 32 heads on 8: 26 us without, 17 with; with many tiles the CTAs'
-// beginnings and ends cost more than it gains).
+// threads of a warp read the same four at a time.  Where there are fewer tiles of keys than SMs, the heads of a group go to CTAs of
+// their own, a cluster, whose first adds up the others' sums; with more the CTAs' beginnings and ends cost more than it gains.  Without
+// and with, in us: 32 heads on 8, 1000 tokens (63 tiles) 23.7 and 16.4, 2000 (126) 43.5 and 42.1, 2500 (157) 53.4 and 57.9, 4096 (256)
+// 95.7 and 119.9, 16384 1354 and 1586; 16 heads on 2, 1000 tokens (16) 43.9 and 12.2, 8192 (128) 305 and 215, 12000 (188) 458 and 447,
+// 16384 (256) 711 and 785; four ragged requests, 32 on 8, 5000 tokens in all, 77 and 120.
 //
 // Bound.  128 x 128 logits are 512 cycles of the tensor cores and 1024 of the special-function unit: a share of the
 // exponentials is computed on the FMA pipe (exp2_poly), until both units are busy.
 //
 // Sums.  A tile's 128 terms are added in fp32, the tiles' sums with their rounding errors kept (two-part sums).
 constexpr int A_GROUPS = 3, A_THREADS = A_GROUPS * 128 + 128, A_BUFS = 4, A_STAGES = 4;
-constexpr int kFewTiles = 2;                     // tiles of keys per SM below which heads are split
 constexpr int A_TMA = A_GROUPS * 4, A_MMA = A_TMA + 1, A_LSE = A_TMA + 2;
 
 template <int D> constexpr size_t acc_smem() {
@@ -735,7 +736,7 @@ int32_t launch_accumulate_tc(const cake_ctx* ctx, const void* q, Strided qs, con
   PromptBatch B;
   for (int lo = 0; lo < ctx->n_req; lo += B.n) {
     fill_prompt_batch(ctx, lo, TILE, B);
-    const bool split = P.G > 1 && B.tiles * P.Hkv < kFewTiles * ctx->n_sm;
+    const bool split = P.G > 1 && B.tiles * P.Hkv < ctx->n_sm;
     CAKE_CUDA_TRY(c.head_dim == 128 ? (split ? run_accumulate_tc<128, true>(ctx, qm, km, B, P, st) : run_accumulate_tc<128, false>(ctx, qm, km, B, P, st))
                                     : (split ? run_accumulate_tc<64, true>(ctx, qm, km, B, P, st) : run_accumulate_tc<64, false>(ctx, qm, km, B, P, st)));
   }
