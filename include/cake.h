@@ -365,8 +365,11 @@ int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_s
  *   q            [n_req][H_q][d], n_req <= 65535
  *   k_cache, v_cache, row_offsets  as cake_compact or cake_decode_begin wrote them: block (r,l) is rows
  *                row_offsets[r*L+l] .. row_offsets[r*L+l+1]-1, [H_kv][len][d]; offsets are read on the device.
- *                (After a cake_decode_step every slot of a block holds a row that the step's token has seen,
- *                the evicted one among them: this call then gives that token's attention output.)
+ *                After a cake_decode_step every slot of a block holds a row that the step's token has seen,
+ *                the evicted one among them: this call then gives that token's attention output.
+ *                Before a layer's first step the free slot of every head of a decode cache holds a row of
+ *                zeros, which this call, knowing the offsets alone, attends like any other (a logit of 0 and
+ *                a value of 0): step first, or attend the packed cache
  *   k_tail, v_tail, tail_len, tail_capacity  rows of tokens generated since the compaction, the new one
  *                included: device [n_req][H_kv][tail_capacity][d], of which request r's first tail_len[r]
  *                (device int32, taken as 0 .. tail_capacity) are attended; what lies behind has no

@@ -399,7 +399,8 @@ class Cake:
                      ) -> Tuple[torch.Tensor, torch.Tensor]:
         """Attention of one new token per request, q [n_req][H_q][d], over one layer of the packed cache that compact or
         decode_begin returned (k_cache, v_cache of the same [rows][d]), and over the first tail_len[r] rows of k_tail, v_tail [n_req][H_kv][capacity][d]:
-        (out, lse [n_req][H_q]).  Does not depend on the context's current batch."""
+        (out, lse [n_req][H_q]).  Does not depend on the context's current batch.  A decode cache must have had a step of the
+        layer: before it every head's free slot, a row of zeros, would be attended too."""
         c = self.cfg
         rc, out, lse = _fast.attend_cache(self._a, self._fp32, layer, c.n_layers, c.n_q_heads, c.n_kv_heads, c.head_dim, q,
                                           row_offsets, k_tail, v_tail, tail_len, out, lse, k_cache, v_cache)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle import cake_oracle as O
+from paper_2503_12491_b200 import harness, synth
 from paper_2503_12491_b200.binding import CAKE_ERR_ARG, CAKE_ERR_TIMEOUT
 from test_gpu_attend import BF16, FP32, U, cached, check_cached, check_out, context, f64, prompt, run_cached, weight_error
 
@@ -237,3 +238,34 @@ def test_waits_that_run_out_leave_the_context_usable(d, dtype):
         assert ran_out or i == 1 or dtype == FP32
         cake.begin(cu)
         assert all(same(c(), w) for c, w in zip(calls, good)) and cake.status() == 0
+
+
+# ------------------------------------------------------------------ decode caches
+def test_a_decode_cache_before_and_after_its_first_step():
+    """Before a layer's first step the free slots are rows of zeros, and attended; after it they hold the new token's rows."""
+    d, hq, hkv, L, sw = 64, 4, 2, 2, 8
+    w = synth.scaled(synth.workload(3), n_layers=L, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, seq_lens=(100, 60), total_budget=L * 30,
+                     window=sw)
+    qs, ks, vs = harness.device_inputs(w)
+    cake = harness.cake_for(w)
+    packed = cake.run(qs, ks, vs, w.cu_seqlens)
+    kc, vc, off = cake.decode_begin(ks, vs)
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(2, h, d, generator=g).bfloat16().cuda() for h in (hq, hkv, hkv))
+    o, p = off.cpu().numpy(), packed[2].cpu().numpy()
+
+    def check(got, extra_k, extra_v):
+        for r in range(2):
+            n = (o[r * L + 1] - o[r * L]) // hkv
+            assert (p[r * L + 1] - p[r * L]) // hkv == n - 1
+            for h in range(hkv):
+                rows = slice(p[r * L] + h * (n - 1), p[r * L] + (h + 1) * (n - 1))
+                kn = np.concatenate([f64(packed[0][rows]), extra_k[r, h][None]])
+                vn = np.concatenate([f64(packed[1][rows]), extra_v[r, h][None]])
+                heads = slice(2 * h, 2 * h + 2)
+                check_out(f64(got[0])[r, heads], f64(got[1])[r, heads], O.attend(f64(q)[r, heads], kn, vn),
+                          weight_error(f64(q)[r, heads], kn, d), n, BF16)
+
+    check(cake.attend_cache(0, q, kc, vc, off), np.zeros((2, hkv, d)), np.zeros((2, hkv, d)))
+    cake.decode_step(0, q, k, v, kc, vc)
+    check(cake.attend_cache(0, q, kc, vc, off), f64(k), f64(v))
