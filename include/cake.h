@@ -323,7 +323,11 @@ int32_t cake_decode_get_state(cake_ctx* ctx, int32_t req, int32_t layer, int32_t
  * The attention whose keys the calls above score, shrink and pack: of whole prompts (Section 2, Eq. 2),
  * of new tokens over what was retained, and the attention weight that keys have accumulated (the
  * indicator of the heavy-hitter method in the paper's compatibility study, Section 5.3).  The scale is
- * 1 / sqrt(d).  Softmax statistics, sums and outputs are held in fp32 and rounded once at the end.
+ * 1 / sqrt(d).  Softmax statistics, sums and outputs are held in fp32 and rounded once at the end.  With bf16
+ * inputs the weights are operands of bf16 products, after their sum was taken: rounded to bf16 for prompts,
+ * and over packed rows with more than four query heads per KV head; in two bf16 terms, 2^-16 relative, over
+ * packed rows with up to four, and over 4-bit rows (there times a scale).  The prompts' logits are summed by
+ * the tensor cores, which cut: log-sum-exps are about 1e-7 of the logits' size too small.
  * These calls do not advance the context's batch: they may come at any point of it, on any stream, and
  * several times.  They allocate nothing, synchronise nothing, and a stream capture may record them.  A bounded wait
  * that runs out in one of their kernels shows in cake_status as CAKE_ERR_TIMEOUT, as elsewhere.
@@ -355,7 +359,8 @@ int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, 
  *   A_j = 1/G sum_h sum_{i >= j} exp(q_hi . k_j / sqrt(d) - lse_hi)
  * q, k and lse as in cake_attend_prompt (lse as that call leaves it); out [H_kv][T] fp32.  For an eviction by
  * accumulated attention hand it to cake_set_indicators (with preferences from cake_set_preferences).  The sums do
- * not depend on scheduling: a call repeats bit for bit. */
+ * not depend on scheduling: a call repeats bit for bit.  (From that call's log-sum-exps, whose cut is this one's,
+ * they are 1e-7 off; from log-sum-exps in 64 bits up to 2e-6, all too small.) */
 int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
                                   const void* k, const float* lse, float* out, void* stream);
 

@@ -28,9 +28,12 @@
 // pace).  Channels and keys are taken in whatever order the words bring them, the same one in both operands; a value tile's 16
 // channels come from one group of 32, which has one scale per row.
 //
-// Bound.  bf16 and fp32 rows: DRAM, 5.9 TB/s of the 6.5 that a copy reaches (76 us for 32 requests of 1000 to 6000 rows, 8 heads).  4-bit
-// rows: a unit of 32 rows and 128 channels is about 1050 instructions of a warp, half of them logical operations or additions of
-// whole numbers at two cycles each, and 72 products at eight: 2.7 TB/s (78 us for 32 requests of 1000 to 8000 rows; 32 us of DRAM).
+// Bound, for 8 KV heads of 32 query heads.  bf16 rows: DRAM, 5.8 TB/s of the 6.5 that a copy reaches (75 us for 32 requests of 1000 to
+// 6000 rows of 128 channels; 64 channels 4.4, 49 us).  fp32 rows: three warps per SM with chains of FMA
+// behind reads of shared memory (a 16-byte piece of a query per four of them): 5.1 TB/s (172 us; 64 channels 3.0, 148 us).  4-bit rows, bf16 queries: a unit of 32 rows and 128 channels
+// is about 1050 instructions of a warp, half of them logical operations or additions of whole numbers at two cycles each, 1050 cycles of
+// that pipe, beside 56 products at eight (112 with more than four heads), 450 of the tensor cores: 2.7 TB/s (78 us for 32 requests of
+// 1000 to 8000 rows; 32 us of DRAM).  4-bit rows, fp32 queries: FMA and conversions of codes, 1.3 TB/s (166 us of the same rows).
 #include "cache_mma.cuh"
 #include "tc_ptx.cuh"
 
@@ -100,7 +103,8 @@ struct Requests {
     }
     upto = lanes_before(units, lane);
   }
-  // All of them, the first ones last (they stay); each(base) after every 32.
+  // All of them, the first ones last (they stay); each(base) after every 32.  (A trip to memory per 32 requests, in both kernels: 8192
+  // requests of one row take 0.31 ms for that, 65 535 2.9.)
   template <typename F>
   __device__ __forceinline__ void read_all(const CacheParams& c, int n_req, int lane, F each) {
     all = 0;
@@ -939,7 +943,8 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           dense32_unit<D, HEADS, C::TAIL>(R, qs, st, st + C::TAIL * D * 4, valid, c.scale2, sp, lane);
         }
       }
-      if ((late = !open_place())) break;
+      late = !open_place();
+      if (late) break;
 #pragma unroll
       for (int h = 0; h < HEADS; ++h) {
 #pragma unroll
@@ -996,7 +1001,8 @@ __global__ void __launch_bounds__(W * 32, 1) attend_units(const RowsParams P) {
           }
         }
       }
-      if ((late = !open_place())) break;
+      late = !open_place();
+      if (late) break;
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) {
         R.sum[0] += __shfl_xor_sync(0xffffffffu, R.sum[0], x);
@@ -1177,10 +1183,12 @@ cudaError_t run_units(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st)
 
 template <typename T, int D, int GROUP>
 cudaError_t run_rows(const cake_ctx* ctx, const RowsParams& P, cudaStream_t st) {
-  // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB, fp32 rows 3 x 2 of up to
-  // 32 KB, 4-bit rows of 128 channels 8 x 3 of 5 to 6 KB (12 x 2: one request of 144000 rows 5 % faster, 32 ragged ones as fast,
-  // one of 4096 rows and 256 of 560 4 % and eight heads on one 14 % slower; 16 x 2, with 128 registers a thread, 8 % slower), of 64
-  // channels 12 x 2 (8 x 3: 6 % slower).
+  // Warps and stages as shared memory and registers hold them: bf16 rows 4 x 3 stages of 8 to 16 KB (3 x 4: 1 to 17 % slower, all but
+  // one request of 2048 rows; 6 x 2: 32 ragged requests 2 % faster and 14 % with 64 channels, one KV head per query head 7 % and 6 %, but
+  // 256 requests of 350 rows and one of 2048, 128 channels, 3 % slower), fp32 rows 3 x 2 of up to 32 KB (2 x 3: 3 to 43 % slower),
+  // 4-bit rows of 128 channels 8 x 3 of 5 to 6 KB (12 x 2: one request of 144000 rows 5 % faster, 32 ragged ones as fast, one of 4096
+  // rows and 256 of 560 4 % and eight heads on one 14 % slower; 16 x 2, with 128 registers a thread, 8 % slower), of 64 channels 12 x 2
+  // (8 x 3: 6 % slower).
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int W = !GROUP ? (F32 ? 3 : 4) : F32 || D == 128 ? 8 : 12, ST = (GROUP ? D == 128 && !F32 : !F32) ? 3 : 2;
   return P.c.Hq / P.c.Hkv <= 4 ? run_units<T, D, GROUP, true, W, ST>(ctx, P, st) : run_units<T, D, GROUP, false, W, ST>(ctx, P, st);

@@ -4,8 +4,10 @@
 //   accumulate_tc32   A_j = 1/G sum_h sum_{i>=j} exp(q_hi.k_j / sqrt d - lse_hi).
 //
 // An fp32 number is the exact sum of three bf16 ones (its 24 bits, eight at a time: split8), so a product of two fp32 operands
-// is nine bf16 products, of which the six that reach 2^-24 of the result are taken, the smallest first:
+// is nine bf16 products, of which the six largest are taken, the smallest first:
 //     x1 y3 + x3 y1 + x2 y2 + x1 y2 + x2 y1 + x1 y1 ,  summed in fp32 in tensor memory.
+// Terms are cut, not rounded, so x2 is below 2^-7 of x and x3 below 2^-15, of its sign: x2 y3 and x3 y2, which are left out, are
+// below 2^-22 of the product each and make it smaller.
 // Six bf16 products are still five times as fast as one in fp32 FMA: 375 against 74 TFLOP/s of the device's nominal rates.
 // (An infinity among what a row sees may make the row a NaN: its second and third terms are NaN.)
 //
