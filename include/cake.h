@@ -360,7 +360,8 @@ int32_t cake_attend_prompt(cake_ctx* ctx, const void* q, int64_t q_head_stride, 
  * q, k and lse as in cake_attend_prompt (lse as that call leaves it); out [H_kv][T] fp32.  For an eviction by
  * accumulated attention hand it to cake_set_indicators (with preferences from cake_set_preferences).  The sums do
  * not depend on scheduling: a call repeats bit for bit.  (From that call's log-sum-exps, whose cut is this one's,
- * they are 1e-7 off; from log-sum-exps in 64 bits up to 2e-6, all too small.) */
+ * they are 1e-7 off; from log-sum-exps in 64 bits up to 2e-6, mostly too small.  lse is fp32, and a weight is as
+ * exact as that: 6e-8 |lse|, relative.  With logits of 10^7 and more it says nothing.) */
 int32_t cake_accumulate_attention(cake_ctx* ctx, const void* q, int64_t q_head_stride, int64_t q_token_stride,
                                   const void* k, const float* lse, float* out, void* stream);
 

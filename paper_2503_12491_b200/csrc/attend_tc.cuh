@@ -10,10 +10,11 @@ constexpr int TILE = 128;
 constexpr int SLAB = TILE * 128;                 // bytes of 64 bf16 channels of a tile of 128 rows
 constexpr float kRefSlack = 8.f;                 // powers of two that a row's maximum may lie above its reference
 // Weights are 2^(s * scale - ref) in one rounding, and the reference is the rounded product of the largest s: a difference of up to half
-// of a step of the reference, which cancels in output and log-sum-exp as long as it is a power of two that fp32 has.  From 2^29 on,
-// where a step is 64 and other logits have no weight, both terms are multiplied with this factor, which keeps them there.
+// of a step of the reference, which cancels in output and log-sum-exp as long as it is a power of two that fp32 has.  From 2^30 on,
+// where a step is 128, both terms are multiplied with this factor, which keeps the difference below 32.  (Other logits, a step of s
+// away, stay at least 32 below the largest, weights of 2^-32 in place of less.)
 __device__ __forceinline__ float coarse_factor(float ref) {
-  const int k = max(0, (int)(__float_as_uint(ref) >> 23 & 255u) - (127 + 28));
+  const int k = max(0, (int)(__float_as_uint(ref) >> 23 & 255u) - (127 + 29));
   return __uint_as_float((uint32_t)(127 - k) << 23);
 }
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2) {

@@ -55,27 +55,28 @@ def test_prompt_finite_inputs_whose_logits_overflow(dtype, d, bad):
     check_out(f64(out[:, bad:]), f64(lse[:, bad:]), O.prompt_attention(qn, kn, vn), weight_error(qn, kn, d), n, dtype)
 
 
-def huge(dtype, d, n, heads, seed):
-    """Queries +-2^40 and keys 1..n in some order along one channel: logits at least 2^36 apart, of up to 2^45."""
+def huge(dtype, d, n, heads, size, seed):
+    """Queries of +-size and keys 1..n in some order along one channel: logits size / sqrt(d) apart, of up to n times that."""
     g = torch.Generator().manual_seed(seed)
     sign = torch.where(torch.rand(heads, n, generator=g) < 0.5, -1.0, 1.0)
     order = torch.randperm(n, generator=g) + 1.0
     q, k = torch.zeros(heads, n, d), torch.zeros(1, n, d)
-    q[:, :, 1], k[0, :, 1] = sign * 2.0 ** 40, order
+    q[:, :, 1], k[0, :, 1] = sign * size, order
     v = torch.randn(1, n, d, generator=g)
     return q.to(dtype).cuda(), k.to(dtype).cuda(), v.to(dtype).cuda(), sign.numpy(), order.numpy()
 
 
 @DTYPES
 @pytest.mark.parametrize("d", [64, 128])
-def test_huge_logits(dtype, d):
+@pytest.mark.parametrize("size", [2.0 ** 22, 2.0 ** 25, 2.0 ** 27, 2.0 ** 40, 2.0 ** 100], ids=lambda x: f"2^{int(np.log2(x))}")
+def test_huge_logits(dtype, d, size):
     """Logits far beyond the 24 bits of fp32: all the weight is on the largest, and the output is its value.  Prompts, and the last
     queries over the same rows in a cache.  The cache's weight is 2^0 against a sum of 1: bit for bit.  The prompts' is p / p with
     some p: in bf16 the weight is rounded for its product and the output is rounded (2^-8 each); in fp32 six of nine products of
     p and v are taken (the others are below 2^-21 of it together), summed in steps cut at 2^-23 each, and divided (4 u)."""
     tol = 2.01 * 2.0 ** -8 if dtype == BF16 else 2.0 ** -21 + 6 * 2.0 ** -23 + 4 * U
     n, hq = 250, 4                                    # (keys are whole numbers of eight bits: exact in bf16)
-    q, k, v, sign, order = huge(dtype, d, n, hq, seed=d)
+    q, k, v, sign, order = huge(dtype, d, n, hq, size, seed=d)
     cake = context(hq, 1, d, dtype, (n,))
     out, lse = cake.attend_prompt(q, k, v)
     one, one_lse = cake.attend_cache(0, q[:, -1][None].contiguous(), k[0], v[0], torch.tensor([0, n], device="cuda"))
@@ -83,7 +84,7 @@ def test_huge_logits(dtype, d):
     for h in range(hq):
         for i in range(n):
             j = int(np.argmax(sign[h, i] * order[:i + 1]))
-            top = sign[h, i] * order[j] * 2.0 ** 40 / np.sqrt(d)
+            top = sign[h, i] * order[j] * size / np.sqrt(d)
             assert (np.abs(on[h, i] - vn[j]) <= tol * np.abs(vn[j])).all(), (h, i)
             assert abs(float(lse[h, i]) - top) <= 6 * U * abs(top)
         assert torch.equal(one[0, h], v[0, j]) and abs(float(one_lse[0, h]) - top) <= 6 * U * abs(top)
