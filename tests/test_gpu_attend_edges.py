@@ -270,3 +270,47 @@ def test_a_decode_cache_before_and_after_its_first_step():
     check(cake.attend_cache(0, q, kc, vc, off), np.zeros((2, hkv, d)), np.zeros((2, hkv, d)))
     cake.decode_step(0, q, k, v, kc, vc)
     check(cake.attend_cache(0, q, kc, vc, off), f64(k), f64(v))
+
+
+# ------------------------------------------------------------------ beside the path
+@DTYPES
+def test_attention_on_a_stream_beside_the_eviction_path(dtype):
+    """Scoring, eviction and compaction of a batch on one stream and all four attention calls of the same context on another, at the
+    same time: each as by itself.  (The score kernel's CTAs wait for one another, and both sides hold tensor memory.)"""
+    d, hq, hkv, L, sw = 128, 8, 2, 4, 16
+    lens = (1700, 400)
+    cu = [0, 1700, 2100]
+    cake = context(hq, hkv, d, dtype, lens, window=sw, layers=L, budget=L * 80)
+    layers = [prompt(hq, hkv, d, dtype, lens, seed=l) for l in range(L)]
+    qw = [torch.stack([q[:, cu[r + 1] - sw:cu[r + 1]] for r in range(2)]).contiguous() for q, _, _ in layers]
+    ks, vs = [x[1] for x in layers], [x[2] for x in layers]
+    caches = [cached(hq, hkv, d, dtype, (900, 130, 33), group=g, layers=L) for g in (0, 32)]
+
+    def path():
+        cake.begin(cu)
+        for l in range(L):
+            cake.score_layer(l, qw[l], ks[l])
+            cake.allocate(l)
+            cake.evict(l)
+        k, v, off, pos = cake.compact(ks, vs)
+        return off, pos, k, v
+
+    def attention():
+        out, lse = cake.attend_prompt(*layers[0])
+        return out, lse, cake.accumulate_attention(layers[0][0], ks[0], lse), *run_cached(cake, caches[0]), *run_cached(cake, caches[1])
+
+    want, want_path = attention(), path()
+    n = int(want_path[0][-1])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        with torch.cuda.stream(streams[0]):
+            got_path = path()
+        with torch.cuda.stream(streams[1]):
+            for _ in range(6):
+                got.append(attention())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+        assert torch.equal(got_path[0], want_path[0]) and all(torch.equal(a[:n], b[:n]) for a, b in zip(got_path[1:], want_path[1:]))
+    assert cake.status() == 0
